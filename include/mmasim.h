@@ -250,6 +250,78 @@ int mmasim_reference_fp64(const mmasim_model* model, int64_t M, int64_t N, int64
 int mmasim_deviation_stats(const mmasim_model* model, int64_t M, int64_t N, int64_t K, const void* A, const void* B, const void* C,
                            double* stats, void* stream);
 
+/* Scaled 8- and 4-bit operands made on the GPU, and the kernels of a network that stand around the products of such operands.  The paper has
+ * no counterpart; the arithmetic is plain FP32 (fl = one FP32 rounding to nearest even), as a network's own kernels have it, so that what a
+ * unit's arithmetic does to a result can be told from what the formats do.  Formats (`out_fmt`) and what they come with:
+ *   MMASIM_E4M3, MMASIM_E5M2       codes M x K bytes, row_scale: M floats, s = max(fl(max |x| / top), 2^-126), top 448 / 57344;
+ *                                  code = the nearest to fl(x / s), saturating.  For mmasim_gemm_ex's row_scale / col_scale.
+ *   MMASIM_MXE4M3, MMASIM_MXE5M2   codes M x K bytes, sf: M x ceil(K / 32) E8M0 bytes, floor(log2 max |x|) - 8 / 15, at least 2^-127 (a block
+ *                                  of zeros: code 0); code = the nearest to x / sf, saturating.  For opts->sfa / sfb.
+ *   MMASIM_MXF4_GST                codes M x K / 2 bytes, sf as above with floor(log2 max |x|) - 2; K a multiple of 32
+ *   MMASIM_NVF4_GST                codes M x K / 2 bytes, row_scale: M floats, s = max(fl(max of the row / 2688), 2^-100); sf: M x K / 16 UE4M3
+ *                                  bytes, g = the nearest to fl(max |x| / fl(6 s)) within 2^-9 .. 448; code = the nearest to
+ *                                  fl(x / fl(g s)); K a multiple of 32
+ * A row (of a format with row scales) or a block of 32 (of one without) that holds an infinity or a NaN gets a NaN scale (for MMASIM_NVF4_GST
+ * NaN in sf too); its codes are NaN, 0 where the format has none.  A quotient's sign stays on a zero.
+ * Rows: FP32, BF16 or FP16 words (MMASIM_F32, MMASIM_BF16, MMASIM_F16), M >= 0 of them (with M = 0 nothing is read or written), K from 1 to
+ * 32768; leading dimensions in elements, 0 = packed (sf and row_scale always are); pointers aligned to their element, 16 bytes are faster.
+ * All data is on the current device.  Outputs overlap neither each other nor inputs, except as noted: otherwise MMASIM_ERR_INVALID_ARG. */
+int mmasim_quantize(int in_fmt, int out_fmt, int64_t M, int64_t K, const void* x, int64_t ldx, void* codes, int64_t ld_codes, void* sf,
+                    float* row_scale, void* stream);
+
+/* Root-mean-square norm, with the residual's addition in front and quantisation behind:
+ *   h = x + residual, one rounding to the rows' type, stored to residual_out (x itself without a residual; both or neither are given)
+ *   y = fl(fl(h / sqrt(mean of h^2 + eps)) * weight), the sum of squares in FP32; rounded once to the rows' type (out_fmt = fmt), or
+ *       quantised from FP32 as above (sf and row_scale as the format has them)
+ * A row whose sum of squares passes FP32's range (magnitudes of 1.8e19 and more) comes out as zeros.  residual_out may be x or residual (same
+ * address and stride), and so may a plain `out` be. */
+typedef struct {
+    const void* x;
+    const void* residual;       /* or NULL */
+    const void* weight;         /* K words of weight_fmt, or NULL = ones */
+    void* residual_out;
+    void* out;                  /* rows of the rows' type, or codes */
+    void* sf;                   /* MX formats, MMASIM_NVF4_GST; else NULL */
+    float* row_scale;           /* FP8 and MMASIM_NVF4_GST; else NULL */
+    int64_t ldx, ld_residual, ld_residual_out, ld_out;
+    int32_t weight_fmt;         /* the rows' type or MMASIM_F32 */
+    int32_t out_fmt;
+    float eps;                  /* >= 0 */
+} mmasim_rms_norm_args;
+int mmasim_rms_norm(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_args* args, void* stream);
+
+/* Its gradients, a quantised output taken as if it were not (straight through).  With r = 1 / sqrt(mean of h^2 + eps) and g = dy * weight:
+ *   dx = r g - h (r^3 / K) sum(g h) + dresidual     the gradient of x and of residual alike, one rounding to the rows' type
+ *   dweight = sum over the rows of dy h r           one rounding to weight_fmt; zeros for M = 0
+ * h is what the forward pass stored (residual_out, or x).  dweight is the same from run to run: the rows are added in a fixed order, through
+ * `workspace` (device, mmasim_rms_norm_backward_workspace(M, K) bytes, 16-byte aligned; not needed without dweight), whose contents before
+ * and after mean nothing; calls that may run at the same time need one each.  dx may be dy, h or dresidual (same address and stride). */
+typedef struct {
+    const void* dy;
+    const void* h;
+    const void* weight;         /* or NULL = ones */
+    const void* dresidual;      /* the gradient that residual_out has from elsewhere, or NULL */
+    void* dx;
+    void* dweight;              /* K words of weight_fmt, or NULL */
+    void* workspace;
+    uint64_t workspace_bytes;
+    int64_t ld_dy, ld_h, ld_dresidual, ld_dx;
+    int32_t weight_fmt;
+    float eps;
+} mmasim_rms_norm_backward_args;
+uint64_t mmasim_rms_norm_backward_workspace(int64_t M, int64_t K);
+int mmasim_rms_norm_backward(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_backward_args* args, void* stream);
+
+/* A few tokens times 4-bit weights with group scales, without a model's arithmetic (and without quantised activations: the weight-only
+ * product of a network that generates):
+ *   y (T x N) = x (T x K) * (W (N x K) with its scales)^T * row_scale[n]
+ * w_fmt MMASIM_MXF4_GST or MMASIM_NVF4_GST: W packed two per byte as for mmasim_gemm_ex (16-byte aligned, ldw elements a row, a multiple of 32,
+ * 0 = K), sf N x K / 32 E8M0 or N x K / 16 UE4M3 bytes; row_scale N floats or NULL.  fmt: x and y, FP32, BF16 or FP16.  K a multiple of 32.
+ * Products are exact, sums FP32 (some 128 elements at a time truncated below 2^-24 of the largest of them, then rounded additions), one
+ * rounding to the type of y.  T >= 0; every eight tokens in BF16, four in FP16, two in FP32 read the weights once. */
+int mmasim_matvec4(int w_fmt, int fmt, int64_t T, int64_t N, int64_t K, const void* W, int64_t ldw, const void* sf, const float* row_scale,
+                   const void* x, int64_t ldx, void* y, int64_t ldy, void* stream);
+
 /* Issue-rate micro-benchmarks, the roofline denominators (no counterpart in the paper).  Launches `blocks` CTAs of
  * 256 threads; every thread runs `iters` (rounded up to a multiple of 8) times 8 rounds of independent operations of
  * the given kind.  `sink` (device, >= 4 bytes) receives a value that keeps the work alive.  The caller times the

@@ -6,7 +6,8 @@ it), ``.build`` compiles the library in-tree, ``.workloads`` holds the seeded in
 import importlib
 
 _BINDING = ("ARCH", "FMT", "ACC", "FAMILY", "RHO", "Model", "MmasimError", "create_model", "gemm", "gemm_host",
-            "dot_batch", "int_peak", "last_kernel", "last_variant", "library_path", "model_keys", "PEAK_KINDS", "hw_mma", "HW_KINDS", "error_stats", "STAT_NAMES")
+            "dot_batch", "int_peak", "last_kernel", "last_variant", "library_path", "model_keys", "PEAK_KINDS", "hw_mma", "HW_KINDS", "error_stats", "STAT_NAMES",
+            "quantize", "rms_norm", "rms_norm_backward", "matvec4", "Quantized", "QUANTIZED_FORMATS")
 
 
 def __getattr__(name):

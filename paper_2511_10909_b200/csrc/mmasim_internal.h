@@ -162,6 +162,13 @@ size_t deviation_scratch(int64_t M, int64_t N, int64_t K);
 int launch_deviation_start(int fmt, int64_t M, int64_t N, int64_t K, const void* A, const void* B, void* scratch, cudaStream_t stream);
 int launch_deviation_end(int acc, int64_t M, int64_t N, int64_t K, const void* C, const void* D, void* scratch, double* host, cudaStream_t stream);
 int launch_reference_fp64(int fmt, int acc, int64_t M, int64_t N, int64_t K, const void* A, const void* B, const void* C, double* ref, cudaStream_t stream);
+// mmasim_rows.cuh, mmasim_rows_backward.cu, mmasim_matvec4.cu (arguments checked; leading dimensions of args 0 = packed)
+constexpr int64_t ROWS_MAX_K = 32768;           // what a CTA's registers hold of a row
+int launch_rows(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_args& p, bool norm, cudaStream_t stream);
+size_t rms_norm_backward_workspace(int64_t M, int64_t K);
+int launch_rms_norm_backward(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_backward_args& p, cudaStream_t stream);
+int launch_matvec4(bool nv, int fmt, int64_t T, int64_t N, int64_t K, const void* W, int64_t ldw, const void* sf, const float* row_scale,
+                   const void* x, int64_t ldx, void* y, int64_t ldy, cudaStream_t stream);
 // mmasim_peak.cu
 int launch_int_peak(int kind, int64_t blocks, int64_t iters, void* sink, int32_t* ops_per_round, cudaStream_t stream);
 // mmasim_api.cpp

@@ -6,9 +6,11 @@ import fails, and every compute call needs CUDA tensors.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from ctypes import c_int, c_int32, c_int64, c_void_p, c_char_p, POINTER, Structure, byref
+from ctypes import c_float, c_int, c_int32, c_int64, c_uint64, c_void_p, c_char_p, POINTER, Structure, byref
+from typing import Any, NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmmasim.so")
@@ -43,6 +45,17 @@ class _GemmOpts(Structure):
     _fields_ = [("lda", c_int64), ("ldb", c_int64), ("ldc", c_int64), ("ldd", c_int64),
                 ("sfa", c_void_p), ("sfb", c_void_p), ("k_chunk", c_int64),
                 ("row_scale", c_void_p), ("col_scale", c_void_p), ("flags", c_int32)]
+
+
+class _RmsNormArgs(Structure):
+    _fields_ = [(n, c_void_p) for n in ("x", "residual", "weight", "residual_out", "out", "sf", "row_scale")] \
+        + [(n, c_int64) for n in ("ldx", "ld_residual", "ld_residual_out", "ld_out")] \
+        + [("weight_fmt", c_int32), ("out_fmt", c_int32), ("eps", c_float)]
+
+
+class _RmsNormBackwardArgs(Structure):
+    _fields_ = [(n, c_void_p) for n in ("dy", "h", "weight", "dresidual", "dx", "dweight", "workspace")] + [("workspace_bytes", c_uint64)] \
+        + [(n, c_int64) for n in ("ld_dy", "ld_h", "ld_dresidual", "ld_dx")] + [("weight_fmt", c_int32), ("eps", c_float)]
 
 
 def _load():
@@ -83,6 +96,16 @@ def _load():
     lib.mmasim_reference_fp64.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.mmasim_deviation_stats.restype = c_int
     lib.mmasim_deviation_stats.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.mmasim_quantize.restype = c_int
+    lib.mmasim_quantize.argtypes = [c_int, c_int, c_int64, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+    lib.mmasim_rms_norm.restype = c_int
+    lib.mmasim_rms_norm.argtypes = [c_int, c_int64, c_int64, POINTER(_RmsNormArgs), c_void_p]
+    lib.mmasim_rms_norm_backward.restype = c_int
+    lib.mmasim_rms_norm_backward.argtypes = [c_int, c_int64, c_int64, POINTER(_RmsNormBackwardArgs), c_void_p]
+    lib.mmasim_rms_norm_backward_workspace.restype = c_uint64
+    lib.mmasim_rms_norm_backward_workspace.argtypes = [c_int64, c_int64]
+    lib.mmasim_matvec4.restype = c_int
+    lib.mmasim_matvec4.argtypes = [c_int, c_int, c_int64, c_int64, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
     lib.mmasim_host_release.restype = c_int
     lib.mmasim_host_release.argtypes = []
     lib.mmasim_last_kernel.restype = c_char_p
@@ -104,7 +127,7 @@ class _NoFast:
     def gemm(*args):
         return None
 
-    dot_batch = gemm
+    dot_batch = quantize = rms_norm = rms_norm_backward = matvec4 = gemm
 
 
 def _load_fast(path=os.path.join(_HERE, "_mmasim_py.so")):
@@ -119,10 +142,13 @@ def _load_fast(path=os.path.join(_HERE, "_mmasim_py.so")):
         spec.loader.exec_module(mod)
         if mod.built_against != "torch " + torch.__version__:
             raise ImportError(f"it was built against {mod.built_against}, this is torch {torch.__version__}")
-        mod.bind(*(ctypes.cast(f, c_void_p).value for f in (_lib.mmasim_gemm_ex, _lib.mmasim_dot_batch, _lib.mmasim_model_info)))
+        address = lambda f: ctypes.cast(f, c_void_p).value
+        mod.bind(*map(address, (_lib.mmasim_gemm_ex, _lib.mmasim_dot_batch, _lib.mmasim_model_info)))
+        mod.bind_rows(*map(address, (_lib.mmasim_quantize, _lib.mmasim_rms_norm, _lib.mmasim_rms_norm_backward, _lib.mmasim_rms_norm_backward_workspace,
+                                     _lib.mmasim_matvec4)))
     except (ImportError, OSError, AttributeError) as e:
         import warnings
-        warnings.warn(f"{path} cannot be used ({e}): every gemm and dot_batch call takes some 12 us longer; build it with "
+        warnings.warn(f"{path} cannot be used ({e}): every gemm, dot_batch, quantize, rms_norm and matvec4 call takes some 12 us longer; build it with "
                       "`python -m paper_2511_10909_b200.build`", RuntimeWarning, stacklevel=3)
         mod = _NoFast
     _fast = mod
@@ -473,6 +499,212 @@ def hw_umma(kind: str, A, B, C=None, out=None, *, sfa=None, sfb=None, K=None, st
     code = int(status.item())
     if code:
         raise MmasimError(code, "mmasim_hw_umma: the bounded wait for the instruction ran out; nothing was stored")
+    return out
+
+
+# ---- scaled operands made on the GPU, and the kernels around their products ----
+SCALE_BLOCK = {"mxe4m3": 32, "mxe5m2": 32, "mxf4": 32, "nvf4": 16}
+QUANTIZED_FORMATS = ["e4m3", "e5m2", "mxe4m3", "mxe5m2", "mxf4", "nvf4"]
+_ROW_SCALED = ("e4m3", "e5m2", "nvf4")
+
+
+class Quantized(NamedTuple):
+    """A matrix as gemm takes its operands: ``codes`` (M x K bytes, M x K / 2 for the FP4 formats), ``sf`` (scale bytes, M x ceil(K / block),
+    for sfa / sfb; None for "e4m3" and "e5m2") and ``row_scale`` (M floats, for row_scale / col_scale; None for the MX formats)."""
+    codes: Any
+    sf: Any
+    row_scale: Any
+
+
+@contextlib.contextmanager
+def _launching(dev, stream):
+    """The raw stream of a call on ``dev``; what is allocated meanwhile belongs to that stream."""
+    import torch
+    if stream is None:
+        with torch.cuda.device(dev):
+            yield c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        if stream.device != dev:
+            raise MmasimError(1, f"the stream is on {stream.device}, the tensors are on {dev}")
+        with torch.cuda.stream(stream):
+            yield c_void_p(stream.cuda_stream)
+
+
+def _row_format(t, name):
+    import torch
+    f = {torch.float32: "fp32", torch.bfloat16: "bf16", torch.float16: "fp16"}.get(t.dtype)
+    if f is None:
+        raise MmasimError(1, f"{name} must be FP32, BF16 or FP16, it is {t.dtype}")
+    return FMT[f]
+
+
+def _rows(t, name, rows, cols, dtype, device):
+    """Checks one matrix of exactly rows x cols and returns its leading dimension in its own elements."""
+    if not t.is_cuda or t.device != device:
+        raise MmasimError(1, f"{name} must be a CUDA tensor on {device} (no CPU fallback)")
+    if t.dtype != dtype:
+        raise MmasimError(1, f"{name} must be {dtype}, it is {t.dtype}")
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise MmasimError(3, f"{name} has shape {tuple(t.shape)}, the call needs {rows} x {cols}")
+    if cols > 1 and t.stride(1) != 1 and t.numel():
+        raise MmasimError(3, f"{name} must be contiguous along its rows (stride {t.stride(1)})")
+    if rows > 1 and t.stride(0) < cols:
+        raise MmasimError(3, f"{name}: row stride {t.stride(0)} is smaller than the row length {cols}")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _row_matrix(x, name):
+    if not x.is_cuda or x.dim() != 2:
+        raise MmasimError(1 if not x.is_cuda else 3, f"{name} must be a CUDA matrix (no CPU fallback)")
+    return x.shape[0], x.shape[1], x.device, _row_format(x, name)
+
+
+def _packed_vector(t, name, shape, dtype, device):
+    if not t.is_cuda or t.device != device or t.dtype != dtype:
+        raise MmasimError(1, f"{name} must be a {dtype} CUDA tensor on {device}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise MmasimError(3, f"{name} must be a contiguous tensor of shape {shape}, it has {tuple(t.shape)}")
+
+
+def _weight_format(w, name, K, x_fmt, x, dev):
+    import torch
+    if w is None:
+        return x_fmt
+    _packed_vector(w, name, (K,), w.dtype, dev)
+    if w.dtype not in (x.dtype, torch.float32):
+        raise MmasimError(1, f"{name} must be {x.dtype} or FP32, it is {w.dtype}")
+    return FMT["fp32"] if w.dtype == torch.float32 else x_fmt
+
+
+def _quantized_buffers(out, fmt, M, K, dev):
+    """The three buffers of a quantised matrix, ``out``'s or new ones, and the leading dimension of the codes in elements."""
+    import torch
+    if fmt not in QUANTIZED_FORMATS:
+        raise MmasimError(2, f"the formats are {', '.join(QUANTIZED_FORMATS)}; got {fmt!r}")
+    per_byte = 2 if fmt in ("mxf4", "nvf4") else 1
+    if per_byte == 2 and K % 32:
+        raise MmasimError(3, f"{fmt} needs K to be a multiple of 32, it is {K}")
+    block = SCALE_BLOCK.get(fmt)
+    sf_shape = (M, -(-K // block)) if block else None
+    if out is None:
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=dev)
+        out = Quantized(new((M, K // per_byte), torch.uint8), new(sf_shape, torch.uint8) if block else None,
+                        new((M,), torch.float32) if fmt in _ROW_SCALED else None)
+    codes, sf, row_scale = out
+    ld = _rows(codes, "codes", M, K // per_byte, torch.uint8, dev) * per_byte
+    if (sf is None) != (block is None) or (row_scale is None) != (fmt not in _ROW_SCALED):
+        raise MmasimError(1, f"{fmt} has {'no ' if block is None else ''}sf and {'no ' if fmt not in _ROW_SCALED else ''}row_scale")
+    if sf is not None:
+        _packed_vector(sf, "sf", sf_shape, torch.uint8, dev)
+    if row_scale is not None:
+        _packed_vector(row_scale, "row_scale", (M,), torch.float32, dev)
+    return Quantized(codes, sf, row_scale), ld
+
+
+def quantize(x, fmt: str, out: Quantized | None = None, *, stream=None) -> Quantized:
+    """The rows of ``x`` (FP32, BF16 or FP16, M x K, row-strided) as codes and scales of ``fmt``, one of QUANTIZED_FORMATS (mmasim_quantize):
+    "e4m3" / "e5m2" with a scale per row, "mxe4m3" / "mxe5m2" / "mxf4" with one per 32 elements, "nvf4" with one per 16 and one per row.
+    ``out``: a Quantized of buffers to write to."""
+    if stream is None:
+        q = (_fast or _load_fast()).quantize(x, FMT.get(fmt, -1), *(out or (None, None, None)))
+        if q is not None:
+            return Quantized(*q)
+    M, K, dev, x_fmt = _row_matrix(x, "x")
+    ldx = _rows(x, "x", M, K, x.dtype, dev)
+    with _launching(dev, stream) as s:
+        q, ld = _quantized_buffers(out, fmt, M, K, dev)
+        _check(_lib.mmasim_quantize(x_fmt, FMT[fmt], M, K, _ptr(x), ldx, _ptr(q.codes), ld, _ptr(q.sf), _ptr(q.row_scale), s))
+    return q
+
+
+def rms_norm(x, weight=None, residual=None, *, eps: float = 1e-6, fmt: str | None = None, residual_out=None, out=None, stream=None):
+    """Root-mean-square norm of the rows of ``x`` (mmasim_rms_norm): h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight.
+    Returns (y, h): y in x's type, or a Quantized of ``fmt``; h is None without a residual.  ``residual_out`` and ``out`` (a tensor, or a
+    Quantized) are written to if given; residual_out may be x or residual, an ``out`` in x's type too.  The weight is of x's type or FP32."""
+    if stream is None:
+        quantised = fmt is not None
+        bufs = (out if quantised and out is not None else (None, None, None)) if quantised else (out, None, None)
+        r = (_fast or _load_fast()).rms_norm(x, weight, residual, eps, FMT.get(fmt, -1) if quantised else -2, residual_out, *bufs)
+        if r is not None:
+            return (Quantized(*r[:3]) if quantised else r[0]), r[3]
+    import torch
+    M, K, dev, x_fmt = _row_matrix(x, "x")
+    a = _RmsNormArgs(eps=eps, out_fmt=x_fmt, x=x.data_ptr(), ldx=_rows(x, "x", M, K, x.dtype, dev), weight_fmt=_weight_format(weight, "weight", K, x_fmt, x, dev))
+    a.weight = None if weight is None else weight.data_ptr()
+    if residual_out is not None and residual is None:
+        raise MmasimError(1, "residual_out without a residual")
+    with _launching(dev, stream) as s:
+        if residual is not None:
+            a.residual, a.ld_residual = residual.data_ptr(), _rows(residual, "residual", M, K, x.dtype, dev)
+            if residual_out is None:
+                residual_out = torch.empty((M, K), dtype=x.dtype, device=dev)
+            a.residual_out, a.ld_residual_out = residual_out.data_ptr(), _rows(residual_out, "residual_out", M, K, x.dtype, dev)
+        if fmt is None:
+            y = torch.empty((M, K), dtype=x.dtype, device=dev) if out is None else out
+            a.out, a.ld_out = y.data_ptr(), _rows(y, "out", M, K, x.dtype, dev)
+        else:
+            y, a.ld_out = _quantized_buffers(out, fmt, M, K, dev)
+            a.out, a.out_fmt = y.codes.data_ptr(), FMT[fmt]
+            a.sf = None if y.sf is None else y.sf.data_ptr()
+            a.row_scale = None if y.row_scale is None else y.row_scale.data_ptr()
+        _check(_lib.mmasim_rms_norm(x_fmt, M, K, byref(a), s))
+    return y, residual_out
+
+
+def rms_norm_backward(dy, h, weight=None, dresidual=None, *, eps: float = 1e-6, need_dweight: bool = True, dx=None, stream=None):
+    """Gradients of rms_norm (mmasim_rms_norm_backward): (dx, dweight) from the gradient ``dy`` of its output (a quantised output counts as
+    if it were not), the rows ``h`` that it stored and the gradient ``dresidual`` that they have from elsewhere.  dx is the gradient of x and
+    of the residual alike; dweight is of the weight's type (without one: of h's), None with ``need_dweight`` false."""
+    if stream is None:
+        r = (_fast or _load_fast()).rms_norm_backward(dy, h, weight, dresidual, eps, need_dweight, dx)
+        if r is not None:
+            return r
+    import torch
+    M, K, dev, fmt = _row_matrix(h, "h")
+    a = _RmsNormBackwardArgs(eps=eps, dy=dy.data_ptr(), ld_dy=_rows(dy, "dy", M, K, h.dtype, dev), h=h.data_ptr(), ld_h=_rows(h, "h", M, K, h.dtype, dev))
+    a.weight_fmt = _weight_format(weight, "weight", K, fmt, h, dev)
+    a.weight = None if weight is None else weight.data_ptr()
+    if dresidual is not None:
+        a.dresidual, a.ld_dresidual = dresidual.data_ptr(), _rows(dresidual, "dresidual", M, K, h.dtype, dev)
+    with _launching(dev, stream) as s:
+        if dx is None:
+            dx = torch.empty((M, K), dtype=h.dtype, device=dev)
+        a.dx, a.ld_dx = dx.data_ptr(), _rows(dx, "dx", M, K, h.dtype, dev)
+        dweight = workspace = None
+        if need_dweight:
+            dweight = torch.empty((K,), dtype=h.dtype if weight is None else weight.dtype, device=dev)
+            a.workspace_bytes = _lib.mmasim_rms_norm_backward_workspace(M, K)
+            workspace = torch.empty((a.workspace_bytes,), dtype=torch.uint8, device=dev)
+            a.dweight, a.workspace = dweight.data_ptr(), workspace.data_ptr()
+        _check(_lib.mmasim_rms_norm_backward(fmt, M, K, byref(a), s))
+    return dx, dweight
+
+
+def matvec4(fmt: str, W, sf, x, row_scale=None, *, out=None, stream=None):
+    """y = x W^T for a few tokens ``x`` (T x K; FP32, BF16 or FP16) and 4-bit weights ``W`` (N x K / 2 bytes, "mxf4" or "nvf4") with their
+    scales ``sf`` and, where they have them, ``row_scale``, as quantize lays them out (mmasim_matvec4): T x N of x's type, sums in FP32."""
+    if stream is None:
+        y = (_fast or _load_fast()).matvec4(FMT.get(fmt, -1), W, sf, x, row_scale, out)
+        if y is not None:
+            return y
+    import torch
+    if fmt not in ("mxf4", "nvf4"):
+        raise MmasimError(2, f"the weights of matvec4 are mxf4 or nvf4; got {fmt!r}")
+    T, K, dev, x_fmt = _row_matrix(x, "x")
+    if K % 32 or not K:
+        raise MmasimError(3, f"K must be a multiple of 32, it is {K}")
+    if W.dim() != 2:
+        raise MmasimError(3, f"W must be a matrix, it has {W.dim()} dimensions")
+    N = W.shape[0]
+    ldx, ldw = _rows(x, "x", T, K, x.dtype, dev), _rows(W, "W", N, K // 2, torch.uint8, dev) * 2
+    _packed_vector(sf, "sf", (N, K // SCALE_BLOCK[fmt]), torch.uint8, dev)
+    if row_scale is not None:
+        _packed_vector(row_scale, "row_scale", (N,), torch.float32, dev)
+    with _launching(dev, stream) as s:
+        if out is None:
+            out = torch.empty((T, N), dtype=x.dtype, device=dev)
+        ldy = _rows(out, "out", T, N, x.dtype, dev)
+        _check(_lib.mmasim_matvec4(FMT[fmt], x_fmt, T, N, K, _ptr(W), ldw, _ptr(sf), _ptr(row_scale), _ptr(x), ldx, _ptr(out), ldy, s))
     return out
 
 
