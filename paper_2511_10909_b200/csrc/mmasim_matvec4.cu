@@ -2,20 +2,33 @@
 //
 //   y[t, n] = row_scale[n] * sum over k of x[t, k] * e2m1(W[n, k]) * sf[n, k / kb]          in FP32
 //
-// What bounds it is reading the weights once: 46 of them per clock and SM at the memory's rate, when 64 lanes of integer work are to be had.
-// So the products go to the warp-level matrix instruction (BF16, exact products, FP32 sums), and the work per weight is its decoding: a code
-// s e e m moves to the sign and the lowest bits of a BF16 word's exponent and significand - a number 2^-126 times its value, subnormals and
-// all - by one mask, one multiplication by two powers of two and one mask for two codes 16 bits apart; a multiplication by the scale times
-// 2^126 (2^118 for UE4M3, whose range would not fit) makes it the weight, exactly: two bits times four at most.
-// x is split into BF16 parts without a rounding (BF16 one, FP16 two, FP32 three), each a column of the instruction.  The instruction's sums
-// truncate below 2^-25 of their largest term, so they are taken over 128 elements and added up in FP32 by rounding additions.
+// What bounds it is reading the weights once: 46 of them per clock and SM at the memory's rate.  The products go to the warp-level matrix
+// instruction (exact products, FP32 sums), 16 rows of weights against columns of x, so that a weight costs its decoding and little else:
+// in FP16 one conversion for two codes and one multiplication for two scales, both exact (E2M1 times UE4M3 has six bits; the E8M0 scales of
+// four neighbouring blocks enter relative to their largest, which is applied to the sum).  64 weights of a lane take about 105 instructions;
+// with the codes shifted into place for BF16 they took 190, and that bound the kernel (28672 x 8192, one token: 52 us).
+//
+// x is staged once per CTA in shared memory, a column of FP16 numbers per token (FP32: three), scaled by a power of two per 128 elements so
+// that the largest is in 2^14 .. 2^15.  Elements of BF16 down to 2^-32 of the largest of their 128 are exact that way, of FP32 to 2^-39.
+// 128 elements of which one is not exact go through BF16 and its wider exponents instead, from x itself (FP32: three parts), with the
+// codes moved to the lowest bits of a BF16 word's exponent - a number 2^-126 times its value.
+// The instruction's sums truncate below 2^-24 of their largest term, so they are taken over 128 elements and added up in FP32.
+//
+// One CTA an SM walks over tiles of 16 rows; its warps split K (128 elements in turn) among the 32, 16, 8 or 4 of them that share a tile, by
+// how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next step in flight, over
+// the ends of tiles too.
+#include <type_traits>
 #include "mmasim_quant.cuh"
 
 namespace mmasim {
 namespace {
 using namespace quant;
 
-constexpr int WARPS = 8, ROWS = 16, SMEM_X = 32768;
+constexpr int ROWS = 16, STEP = 256, HALF = 128;        // elements of K that a warp takes at a time, and that share a scale of x
+constexpr int WARPS = 16;                   // of a CTA, the only one of its SM
+constexpr int STAGE = 2304;                 // bytes of a warp's loads of one step: two blocks of 32 weights of two rows for every lane, 16 rows' scale codes
+constexpr int BLOCK_TOKENS = 2;             // up to so many tokens in columns by block
+constexpr size_t SMEM_MOST = 227 * 1024;
 
 struct MatvecArgs {
     int N, K, tokens;
@@ -24,167 +37,715 @@ struct MatvecArgs {
     const void* x;
     void* y;
     int64_t ldw, ldx, ldy;                  // ldw in bytes
-    int slice;                              // chunks of 32 elements whose x is in shared memory at a time, a multiple of 4
-    int vec_x;
+    int vec_x, stages, copy_codes;
 };
 
-// x = the sum of its BF16 parts: truncations of what is left (an infinity or NaN: the first part alone).
-template <int PARTS> __device__ __forceinline__ void split(float v, uint32_t (&part)[PARTS]) {
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-        const uint32_t u = __float_as_uint(v);
-        if ((u & 0x7F800000u) == 0x7F800000u) {
-            part[p] = u >> 16 | (u & 0xFFFFu ? 0x40u : 0u);         // (a NaN stays one)
-            v = 0.0f;
-        } else {
-            part[p] = u >> 16;
-            v = __fsub_rn(v, __uint_as_float(u & 0xFFFF0000u));
-        }
-    }
+template <int T> constexpr int PARTS = T == EF_F32 ? 3 : 1;
+
+// Shared memory: x, a step of zeros, then the scales of its columns, the steps that are not exact in FP16, the warps' shares of a tile, their loads in flight.
+struct Layout {
+    int steps, pitch;                       // pitch: bytes of a column
+    size_t zeros, scales, flags, share, ring, end;
+};
+// A column has HALF_BYTES per 128 elements: four blocks of 32, 16 bytes more behind two of them, and columns 32 bytes off a multiple of 128, so
+// that the eight lanes of a quarter warp (four blocks of two columns) read from different banks.
+constexpr int HALF_BYTES = HALF * 2 + 16;
+__host__ __device__ inline int block_at(int half, int block) { return half * HALF_BYTES + block * 64 + (block >> 1) * 16; }
+__host__ __device__ inline Layout layout(int K, int columns, int nt, int stages) {
+    Layout l;
+    l.steps = (K + STEP - 1) / STEP;
+    l.pitch = (l.steps * (STEP / HALF) * HALF_BYTES + 95) / 128 * 128 + 32;
+    l.zeros = size_t(columns) * l.pitch;    // a step of zeros
+    l.scales = l.zeros + 2 * HALF_BYTES;
+    l.flags = l.scales + size_t(l.steps) * (STEP / HALF) * nt * 8 * 4;
+    l.share = (l.flags + l.steps + 15) / 16 * 16;
+    l.ring = l.share + size_t(WARPS) * ROWS * nt * 8 * 4;
+    l.end = l.ring + size_t(stages) * WARPS * STAGE;
+    return l;
 }
-__device__ __forceinline__ void decode(uint32_t w, uint32_t (&r)[4]) {          // r[j]: codes j (low half) and j + 4
+
+// The tiles and steps of a warp, one after the other: rounds in which groups of `split` warps have a tile each.
+struct Walk {
+    int done, split, tile, part, base;      // this warp's step is base + part, base in steps of split
+    __device__ __forceinline__ void begin(int d, int tiles, int ctas) {
+        done = d;
+        const int rest = tiles - done, warp = threadIdx.x >> 5;
+        split = rest > 7 * ctas ? WARPS / 8 : (rest > 3 * ctas ? WARPS / 4 : (rest > ctas ? WARPS / 2 : WARPS));
+        const int group = warp / split;
+        tile = done + group * ctas + blockIdx.x;
+        part = warp - group * split;
+        base = 0;
+    }
+    __device__ __forceinline__ int step() const { return base + part; }
+    __device__ __forceinline__ int following(int ctas) const { return done + WARPS / split * ctas; }
+};
+
+struct Item {                               // a lane's blocks of 32 weights of two rows, and their scale codes
+    uint4 a, b;
+    uint32_t ca, cb;
+};
+extern __shared__ __align__(128) unsigned char smem[];          // (places in it are 32-bit offsets)
+__device__ __forceinline__ uint4 load16(uint32_t at) { return *reinterpret_cast<const uint4*>(smem + at); }
+// The codes of a block, and of two neighbouring ones (MXF4: in the halves of the word).
+template <bool NV> __device__ __forceinline__ uint32_t load_code(const uint8_t* at) { return NV ? *reinterpret_cast<const unsigned short*>(at) : *at; }
+template <bool NV> __device__ __forceinline__ uint32_t load_codes(const uint8_t* at) {
+    return NV ? *reinterpret_cast<const uint32_t*>(at) : __byte_perm(*reinterpret_cast<const unsigned short*>(at), 0, 0x4140);
+}
+
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) { uint32_t r; asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) { uint32_t r; asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+__device__ __forceinline__ void decode_f16(uint32_t w, uint32_t (&r)[4]) {      // r[j]: codes 2j (low half) and 2j + 1
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
+}
+__device__ __forceinline__ void decode_bf16(uint32_t w, uint32_t (&r)[4]) {     // r[j]: codes j (low half) and j + 4, 2^-126 times their values
     const uint32_t u = w >> 8;
     r[0] = ((w & 0x000F000Fu) * 0x1040u) & 0x81C081C0u;
     r[1] = ((w & 0x00F000F0u) * 0x0104u) & 0x81C081C0u;
     r[2] = ((u & 0x000F000Fu) * 0x1040u) & 0x81C081C0u;
     r[3] = ((u & 0x00F000F0u) * 0x0104u) & 0x81C081C0u;
 }
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
-// E8M0 code -> 2^126 times its value as two equal BF16 words, in two factors where one does not hold it.
-__device__ __forceinline__ void mx_scale(uint32_t code, uint32_t& a, uint32_t& b) {
-    a = code == 255u ? 0x7FC07FC0u : (min(code, 128u) + 126u) * 0x00800080u;
-    b = code == 255u || code <= 128u ? 0x3F803F80u : (code - 1u) * 0x00800080u;      // 2^(code - 128)
-}
-__device__ __forceinline__ uint32_t nv_scale(uint32_t code) {                       // UE4M3 code -> 2^118 times its value
-    const float f = __fmul_rn(ue4m3_value(code & 0x7Fu), 3.32306998946229e35f);     // 2^118
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %1;" : "=r"(r) : "f"(f));
-    return r;
-}
+template <bool BF16>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if constexpr (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ float power(int code) { return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7FC00000u : uint32_t(code) << 23); }      // of an E8M0 code
+
+// A step that FP16 has not exactly, through BF16: x from memory.  Four sums of the lane, of eight columns.
+template <int T, bool NV>
+__device__ __noinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const typename Elem<T>::type* x, int64_t ldx, int vec_x, int columns, int per_token, int first, int k) {
+    uint32_t fa[2], fb[2], more_a = 0x3F803F80u, more_b = 0x3F803F80u;
+    if constexpr (NV) {                                 // 2^118 times the scales: 2^126 times 448 would be too large
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %1;" : "=r"(fa[i]) : "f"(__fmul_rn(ue4m3_value(ca >> (8 * i) & 0x7Fu), 3.32306998946229e35f)));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %1;" : "=r"(fb[i]) : "f"(__fmul_rn(ue4m3_value(cb >> (8 * i) & 0x7Fu), 3.32306998946229e35f)));
+        }
+    } else {                                            // 2^126 times the scales, in two factors where one does not hold it
+        fa[0] = fa[1] = ca == 255u ? 0x7FC07FC0u : (min(ca, 128u) + 126u) * 0x00800080u;
+        fb[0] = fb[1] = cb == 255u ? 0x7FC07FC0u : (min(cb, 128u) + 126u) * 0x00800080u;
+        if (ca != 255u && ca > 128u) more_a = (ca - 1u) * 0x00800080u;
+        if (cb != 255u && cb > 128u) more_b = (cb - 1u) * 0x00800080u;
+    }
+    const int c = first + (int(threadIdx.x & 31) >> 2), tok = c / per_token, part = c % per_token;      // (parts of nothing are zeros)
+    float d[4] = {};
+#pragma unroll 1
+    for (int word = 0; word < 4; ++word) {
+        uint32_t ra[4], rb[4], u[8];
+        decode_bf16(word_of(va, word), ra);
+        decode_bf16(word_of(vb, word), rb);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ra[j] = mul_bf16x2(mul_bf16x2(ra[j], fa[word >> 1]), more_a);
+            rb[j] = mul_bf16x2(mul_bf16x2(rb[j], fb[word >> 1]), more_b);
+        }
+        Pair v[4];
+        widen<T>(load8<T, false>(x + (k >= 0 && c < columns ? tok * ldx + k + word * 8 : 0), k >= 0 && c < columns ? 8 : 0, vec_x), v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                   // the column's part: truncations of what is left; an infinity or NaN is the first alone
+            float even, odd;
+            split(v[i / 2], even, odd);
+            u[i] = __float_as_uint(i & 1 ? odd : even);
+            const bool number = (u[i] & INF_BITS) != INF_BITS;
+            for (int p = 0; p < part; ++p) u[i] = number ? __float_as_uint(__fsub_rn(__uint_as_float(u[i]), __uint_as_float(u[i] & 0xFFFF0000u))) : 0u;
+            u[i] = u[i] >> 16 | (!number && part == 0 && (u[i] & 0xFFFFu) ? 0x40u : 0u);
+        }
+        mma<true>(d, ra[0], rb[0], ra[1], rb[1], u[0] | u[4] << 16, u[1] | u[5] << 16);
+        mma<true>(d, ra[2], rb[2], ra[3], rb[3], u[2] | u[6] << 16, u[3] | u[7] << 16);
+    }
+    constexpr float back = NV ? 256.0f : 1.0f;
+    return make_float4(d[0] * back, d[1] * back, d[2] * back, d[3] * back);
+}
+// A step whose blocks have scales far apart or far out (or NaN), one block of the four at a time, for eight columns.
+__device__ __noinline__ float4 block_sums(uint4 va, uint4 vb, int ca, int cb, uint32_t x, float2 f) {
+    double sum[4] = {};
+#pragma unroll 1
+    for (int one = 0; one < 4; ++one) {
+        const bool mine = int(threadIdx.x & 3) == one;
+        const int from = int(threadIdx.x & 28) + one;
+        const double pa = power(__shfl_sync(0xFFFFFFFFu, ca, from)), pb = power(__shfl_sync(0xFFFFFFFFu, cb, from));
+        float d[4] = {};
+#pragma unroll
+        for (int word = 0; word < 4; ++word) {
+            uint32_t ra[4], rb[4];
+            decode_f16(mine ? word_of(va, word) : 0u, ra);
+            decode_f16(mine ? word_of(vb, word) : 0u, rb);
+            const uint4 b = load16(x + word * 16);
+            mma<false>(d, ra[0], rb[0], ra[1], rb[1], b.x, b.y);
+            mma<false>(d, ra[2], rb[2], ra[3], rb[3], b.z, b.w);
+        }
+        sum[0] += double(d[0]) * f.x * pa;
+        sum[1] += double(d[1]) * f.y * pa;
+        sum[2] += double(d[2]) * f.x * pb;
+        sum[3] += double(d[3]) * f.y * pb;
+    }
+    return make_float4(float(sum[0]), float(sum[1]), float(sum[2]), float(sum[3]));
 }
 
-template <int T, bool NV>
-__global__ void __launch_bounds__(WARPS * 32) matvec4_kernel(const MatvecArgs a) {
+template <bool NV, int NT>
+struct Product {
+    uint32_t x[NT], scales_at;              // where this lane's block of the step is, in the column that it feeds, and the scales of the columns whose sums it has
+    uint32_t x_next, scales_next;           // how far the following step is
+    float acc[NT][4];
+
+    __device__ __forceinline__ void begin(const Layout& l, int columns, int lane, int step, int split) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)     // (columns behind the last have its sums; nobody reads them)
+            x[nt] = min(nt * 8 + (lane >> 2), columns - 1) * l.pitch + block_at(step * 2, lane & 3);
+        scales_at = uint32_t(l.scales) + (lane & 3) * 8 + step * (2 * NT * 32);
+        x_next = split * (2 * HALF_BYTES);
+        scales_next = split * (2 * NT * 32);
+    }
+    __device__ __forceinline__ void next() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x[nt] += x_next;
+        scales_at += scales_next;
+    }
+    __device__ __forceinline__ float2 scales(int half, int nt) const { return *reinterpret_cast<const float2*>(smem + scales_at + (half * NT + nt) * 32); }
+    __device__ __forceinline__ void add(int nt, const float4& v) {
+        acc[nt][0] += v.x; acc[nt][1] += v.y; acc[nt][2] += v.z; acc[nt][3] += v.w;
+    }
+    // d[h] = 16 rows times the columns over each 128 of the step, weights times fa and fb (two halves of a block of 32 each); the two are
+    // independent of one another, and so are the two sums of each, so that the instructions do not wait for one another.
+    __device__ __forceinline__ void sums(const Item (&it)[2], const uint32_t (&fa)[2][2], const uint32_t (&fb)[2][2], float (&d)[2][NT][4]) const {
+        float e[2][NT][4];
+#pragma unroll
+        for (int word = 0; word < 4; ++word) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t ra[4], rb[4];
+                decode_f16(word_of(it[h].a, word), ra);
+                decode_f16(word_of(it[h].b, word), rb);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { ra[j] = mul_f16x2(ra[j], fa[h][word / 2]); rb[j] = mul_f16x2(rb[j], fb[h][word / 2]); }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint4 b = load16(x[nt] + h * HALF_BYTES + word * 16);
+                    if (word == 0) {
+                        mma_first(d[h][nt], ra[0], rb[0], ra[1], rb[1], b.x, b.y);
+                        mma_first(e[h][nt], ra[2], rb[2], ra[3], rb[3], b.z, b.w);
+                    } else {
+                        mma<false>(d[h][nt], ra[0], rb[0], ra[1], rb[1], b.x, b.y);
+                        mma<false>(e[h][nt], ra[2], rb[2], ra[3], rb[3], b.z, b.w);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[h][nt][i] = __fadd_rn(d[h][nt][i], e[h][nt][i]);
+    }
+    __device__ __forceinline__ void step_nv(const Item (&it)[2]) {
+        float d[2][NT][4];
+        uint32_t fa[2][2], fb[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t sa, sb;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(sa) : "h"((unsigned short)(it[h].ca & 0x7F7Fu)));
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(sb) : "h"((unsigned short)(it[h].cb & 0x7F7Fu)));
+            fa[h][0] = __byte_perm(sa, sa, 0x1010); fa[h][1] = __byte_perm(sa, sa, 0x3232);
+            fb[h][0] = __byte_perm(sb, sb, 0x1010); fb[h][1] = __byte_perm(sb, sb, 0x3232);
+        }
+        sums(it, fa, fb, d);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 f = scales(h, nt);
+                acc[nt][0] = __fmaf_rn(d[h][nt][0], f.x, acc[nt][0]);
+                acc[nt][1] = __fmaf_rn(d[h][nt][1], f.y, acc[nt][1]);
+                acc[nt][2] = __fmaf_rn(d[h][nt][2], f.x, acc[nt][2]);
+                acc[nt][3] = __fmaf_rn(d[h][nt][3], f.y, acc[nt][3]);
+            }
+    }
+    // The scales of a row's four blocks enter relative to their largest: from 2^-14 on FP16 has the weights exactly.  Others, those outside
+    // 2^-63 .. 2^102 (whose sums might leave FP32 before x's scale is applied) and NaN go the long way.
+    __device__ __forceinline__ void step_mx(const Item (&it)[2]) {
+        uint32_t fa[2][2], fb[2][2], top[2];
+        bool fine = true;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t c = it[h].ca << 16 | it[h].cb;
+            top[h] = __vmaxu2(c, __shfl_xor_sync(0xFFFFFFFFu, c, 1));
+            top[h] = __vmaxu2(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], 2));
+            const uint32_t up = c + 0x000F000Fu - top[h];           // (at least 1 in both halves where the scales are fine)
+            fine = fine && it[h].ca + 14 >= top[h] >> 16 && it[h].cb + 14 >= (top[h] & 0xFFFFu) && (top[h] >> 16) - 64 <= 165 && (top[h] & 0xFFFFu) - 64 <= 165;
+            fa[h][0] = fa[h][1] = (up >> 16) * 0x04000400u;
+            fb[h][0] = fb[h][1] = (up & 0xFFFFu) * 0x04000400u;
+        }
+        if (!__all_sync(0xFFFFFFFFu, fine)) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const uint4 va = h ? it[1].a : it[0].a, vb = h ? it[1].b : it[0].b;
+                const int ca = h ? it[1].ca : it[0].ca, cb = h ? it[1].cb : it[0].cb;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) add(nt, block_sums(va, vb, ca, cb, x[nt] + h * HALF_BYTES, scales(h, nt)));
+            }
+            return;
+        }
+        float d[2][NT][4];
+        sums(it, fa, fb, d);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float pa = __uint_as_float((top[h] & 0xFF0000u) << 7), pb = __uint_as_float(top[h] << 23);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 f = scales(h, nt);
+                acc[nt][0] = __fmaf_rn(__fmul_rn(d[h][nt][0], pa), f.x, acc[nt][0]);
+                acc[nt][1] = __fmaf_rn(__fmul_rn(d[h][nt][1], pa), f.y, acc[nt][1]);
+                acc[nt][2] = __fmaf_rn(__fmul_rn(d[h][nt][2], pb), f.x, acc[nt][2]);
+                acc[nt][3] = __fmaf_rn(__fmul_rn(d[h][nt][3], pb), f.y, acc[nt][3]);
+            }
+        }
+    }
+};
+
+// The same for few tokens of 16 bits: a token has four columns, one for each of the four blocks of 32 of the 128 elements, with x there and
+// zeros elsewhere.  The sums then come by block, and the scales multiply sums instead of weights: 8 products of a lane for 64.
+template <bool NV, int NT>
+struct BlockProduct {
+    uint32_t x[NT], x_next[NT], scales_at, scales_next;         // where this lane's block of the step is (or zeros), how far the following one is
+    float acc[NT][4];
+
+    __device__ __forceinline__ void begin(const Layout& l, int columns, int lane, int step, int split) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int tok = nt * 2 + (lane >> 4), block = lane & 3;
+            const bool own = (lane >> 2 & 3) == block && tok < columns;
+            x[nt] = own ? tok * l.pitch + block_at(step * 2, block) : uint32_t(l.zeros);
+            x_next[nt] = own ? split * (2 * HALF_BYTES) : 0;
+        }
+        scales_at = uint32_t(l.scales) + (lane >> 1 & 1) * 4 + step * (2 * NT * 32);
+        scales_next = split * (2 * NT * 32);
+    }
+    __device__ __forceinline__ void next() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x[nt] += x_next[nt];
+        scales_at += scales_next;
+    }
+    __device__ __forceinline__ float scale(int half, int nt) const { return *reinterpret_cast<const float*>(smem + scales_at + half * (NT * 32) + nt * 8); }
+    __device__ __forceinline__ void add(int nt, const float4& v) {
+        acc[nt][0] += v.x; acc[nt][1] += v.y; acc[nt][2] += v.z; acc[nt][3] += v.w;
+    }
+    // d[h][s]: of the two sixteens of the blocks of 32, weights without their scales
+    __device__ __forceinline__ void sums(const uint4 (&wa)[2], const uint4 (&wb)[2], float (&d)[2][2][NT][4]) const {
+#pragma unroll
+        for (int word = 0; word < 4; ++word)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t ra[4], rb[4];
+                decode_f16(word_of(wa[h], word), ra);
+                decode_f16(word_of(wb[h], word), rb);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint4 b = load16(x[nt] + h * HALF_BYTES + word * 16);
+                    float (&to)[4] = d[h][word / 2][nt];
+                    if (word % 2 == 0) mma_first(to, ra[0], rb[0], ra[1], rb[1], b.x, b.y);
+                    else mma<false>(to, ra[0], rb[0], ra[1], rb[1], b.x, b.y);
+                    mma<false>(to, ra[2], rb[2], ra[3], rb[3], b.z, b.w);
+                }
+            }
+    }
+    // `codes`: of rows g (0) and g + 8 (1) for this lane's two columns, which are neighbouring blocks: NVF4 four bytes, MXF4 two in 16-bit halves
+    __device__ __forceinline__ void step(const uint4 (&wa)[2], const uint4 (&wb)[2], const uint32_t (&codes)[2][2]) {
+        float d[2][2][NT][4];
+        sums(wa, wb, d);
+        float s[2][2][2][2];                // [half][row][block][sixteen]
+        if constexpr (NV) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    uint32_t lo, hi;
+                    const uint32_t c = codes[h][r] & 0x7F7F7F7Fu;
+                    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(c));
+                    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&lo)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                    s[h][r][0][0] = f0.x; s[h][r][0][1] = f0.y;
+                    s[h][r][1][0] = f1.x; s[h][r][1][1] = f1.y;
+                }
+        } else {
+            uint32_t least = codes[0][0], most = least;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    least = __vminu2(least, codes[h][r]);
+                    most = __vmaxu2(most, codes[h][r]);
+                    s[h][r][0][0] = __uint_as_float(codes[h][r] << 23);
+                    s[h][r][1][0] = __uint_as_float(codes[h][r] << 7 & 0x7F800000u);
+                }
+            // scales outside 2^-63 .. 2^102, whose products with the sums might leave FP32 before x's scale is applied, the smallest, and NaN
+            if ((least & 0xFFFFu) < 64 || least >> 16 < 64 || (most & 0xFFFFu) > 229 || most >> 16 > 229) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const double f = scale(h, nt);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const double v = (double(d[h][0][nt][i]) + double(d[h][1][nt][i])) * f * power(codes[h][i >> 1] >> (i & 1 ? 16 : 0) & 0xFFu);
+                            acc[nt][i] += float(v);
+                        }
+                    }
+                return;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float f = scale(h, nt);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float (&by)[2] = s[h][i >> 1][i & 1];
+                    const float v = NV ? __fmaf_rn(d[h][0][nt][i], by[0], __fmul_rn(d[h][1][nt][i], by[1])) : __fmul_rn(__fadd_rn(d[h][0][nt][i], d[h][1][nt][i]), by[0]);
+                    acc[nt][i] = __fmaf_rn(v, f, acc[nt][i]);
+                }
+            }
+    }
+};
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory"); }
+// Eight elements of a token into its columns, scaled with the others of their 128 (16 threads); false if one of them is not exact in FP16.
+template <int T>
+__device__ __forceinline__ bool stage_x(const Raw<T>& raw, bool in, unsigned char* at, int pitch, float* scale) {
+    constexpr int P = PARTS<T>;
+    if constexpr (T == EF_F16) {
+        if (in) *reinterpret_cast<uint4*>(at) = make_uint4(raw.w[0], raw.w[1], raw.w[2], raw.w[3]);
+        if (in && scale) *scale = 1.0f;
+        return true;
+    } else {
+        Pair p[4];
+        widen<T>(raw, p);
+        uint32_t top = largest(0u, p);
+#pragma unroll
+        for (int s = 8; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+        // The largest times 2^up is in 2^14 .. 2^15, every part's scale a normal number, and no product with 2^up loses a bit (BF16; of FP32,
+        // the parts behind would show it).
+        const int up = min(141 - int(top >> 23), 126 - 12 * (P - 1));
+        const Pair f = both(__uint_as_float(uint32_t(max(up, -126) + 127) << 23));
+        uint32_t lost = up >= -16 && top < INF_BITS ? 0u : 1u, half[P][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float even, odd;
+            split(mul2(p[j], f), even, odd);
+            if constexpr (T == EF_F32) {                // (a subnormal number times 2^up may lose bits)
+                float x0, x1;
+                split(p[j], x0, x1);
+                lost |= uint32_t(even == 0.0f && x0 != 0.0f) | uint32_t(odd == 0.0f && x1 != 0.0f);
+            }
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(half[q][j]) : "f"(odd), "f"(even));
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&half[q][j]));
+                if (q == P - 1) lost |= (__float_as_uint(even) ^ __float_as_uint(back.x)) | (__float_as_uint(odd) ^ __float_as_uint(back.y));
+                else {
+                    even = __fmul_rn(__fsub_rn(even, back.x), 4096.0f);
+                    odd = __fmul_rn(__fsub_rn(odd, back.y), 4096.0f);
+                }
+            }
+        }
+        if (in) {
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                *reinterpret_cast<uint4*>(at + q * pitch) = make_uint4(half[q][0], half[q][1], half[q][2], half[q][3]);
+                if (scale) scale[q] = __uint_as_float(uint32_t(127 - max(up, -126) - 12 * q) << 23);
+            }
+        }
+        return lost == 0u;
+    }
+}
+
+// What the parts of the kernel share.
+template <int T, bool NV, int NT, bool BLOCKS>
+struct Kernel {
     using E = typename Elem<T>::type;
-    constexpr int PARTS = T == EF_BF16 ? 1 : (T == EF_F16 ? 2 : 3);
-    extern __shared__ __align__(128) unsigned char xs[];
-    __shared__ float share[WARPS][ROWS][8];
-    after_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * ROWS + g, ra = min(row0, a.N - 1), rb = min(row0 + 8, a.N - 1);       // (rows behind the last: read again, not stored)
-    const int chunks = a.K / 32, columns = a.tokens * PARTS, pitch = a.slice * 64;
-    const uint8_t *wa = a.w + ra * a.ldw, *wb = a.w + rb * a.ldw;
-    const int per_row = NV ? chunks * 2 : chunks;
-    const uint8_t *sa = a.sf + int64_t(ra) * per_row, *sb = a.sf + int64_t(rb) * per_row;
-    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int c0 = 0; c0 < chunks; c0 += a.slice) {
-        const int here = min(a.slice, chunks - c0), padded = (here + 3) / 4 * 4;
-        if (c0) __syncthreads();
-        for (int i = threadIdx.x; i < a.tokens * padded * 4; i += WARPS * 32) {         // x in the order of the codes' pairs
-            const int tok = i / (padded * 4), q = i % (padded * 4) / 4, word = i & 3;
-            float v[8];
-            widen<T>(load8<T>(static_cast<const E*>(a.x) + tok * a.ldx + (q < here ? (c0 + q) * 32 + word * 8 : 0), q < here ? 8 : 0, a.vec_x), v);
-            uint32_t part[8][PARTS];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) split<PARTS>(v[e], part[e]);
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const int c = tok * PARTS + p;
-                *reinterpret_cast<uint4*>(xs + c * pitch + q * 64 + ((word + q + c) & 3) * 16) =
-                    make_uint4(part[0][p] | part[4][p] << 16, part[1][p] | part[5][p] << 16, part[2][p] | part[6][p] << 16, part[3][p] | part[7][p] << 16);
-            }
-        }
-        __syncthreads();
-        for (int s = warp; s * 4 < here; s += WARPS) {
-            const int q = s * 4 + t;                    // this lane's chunk, of rows g and g + 8
-            uint4 va = make_uint4(0, 0, 0, 0), vb = va;
-            uint32_t ca = 0, cb = 0;
-            if (q < here) {
-                va = *reinterpret_cast<const uint4*>(wa + int64_t(c0 + q) * 16);
-                vb = *reinterpret_cast<const uint4*>(wb + int64_t(c0 + q) * 16);
-                if constexpr (NV) {
-                    ca = reinterpret_cast<const unsigned short*>(sa)[c0 + q];
-                    cb = reinterpret_cast<const unsigned short*>(sb)[c0 + q];
-                } else {
-                    ca = sa[c0 + q];
-                    cb = sb[c0 + q];
+    static constexpr int P = PARTS<T>, PER_TOKEN = BLOCKS ? 4 : P, CODES = NV ? 2 : 1, ROW_CODES = STEP / 32 * CODES, STEP_BYTES = STEP / 2;
+    const MatvecArgs& a;
+    const Layout l;
+    const int lane, warp, g, t, chunks, tiles, ctas;
+    uint32_t ring, ring_end, in, out;                   // stages to be filled and to be read next
+    Walk ahead;
+    const uint8_t *wa, *wb, *codes;                     // of the step that is fetched next
+    int w_next, codes_next;                             // bytes to the warp's following step
+
+    __device__ __forceinline__ explicit Kernel(const MatvecArgs& args)
+        : a(args), l(layout(args.K, args.tokens * P, NT, args.stages)), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g(lane >> 2), t(lane & 3),
+          chunks(args.K / 32), tiles((args.N + ROWS - 1) / ROWS), ctas(gridDim.x) {
+        in = out = ring = uint32_t(l.ring) + warp * (a.stages * STAGE);
+        ring_end = ring + a.stages * STAGE;
+        enter(0);
+    }
+    __device__ __forceinline__ void enter(int done) {   // (rows behind the last: it again, not stored)
+        ahead.begin(done, tiles, ctas);
+        const int first = (ahead.part * 8 + t) * 16;
+        wa = a.w + min(ahead.tile * ROWS + g, a.N - 1) * a.ldw + first;
+        wb = a.w + min(ahead.tile * ROWS + g + 8, a.N - 1) * a.ldw + first;
+        codes = a.sf + int64_t(min(ahead.tile * ROWS + (lane & 15), a.N - 1)) * (chunks * CODES) + ahead.part * ROW_CODES;
+        w_next = ahead.split * STEP_BYTES;
+        codes_next = ahead.split * ROW_CODES;
+    }
+    // The next step's weights on their way: a lane copies what it will read itself, half a warp the codes.  GENERAL: of any K, the codes not
+    // copied unless they can be.
+    template <bool GENERAL> __device__ __forceinline__ void fetch() {
+        if (ahead.done < tiles) {
+            const int step = ahead.step();
+            if (ahead.tile < tiles && step < l.steps) {
+                const uint32_t to = uint32_t(__cvta_generic_to_shared(smem)) + in + lane * 16;
+                int q = 0, r = 64;
+                if (GENERAL && step == l.steps - 1) {   // (blocks behind the last: it again, times zeros of x)
+                    q = (min(step * 8 + t, chunks - 1) - (step * 8 + t)) * 16;
+                    r = (min(step * 8 + 4 + t, chunks - 1) - (step * 8 + t)) * 16;
+                }
+                copy16(to, wa + q);
+                copy16(to + 512, wa + r);
+                copy16(to + 1024, wb + q);
+                copy16(to + 1536, wb + r);
+                if (lane < 16 && (!GENERAL || a.copy_codes)) {
+                    if constexpr (NV) copy16(to + 2048, codes);
+                    else copy8(to + 2048 - lane * 8, codes);
                 }
             }
-            uint32_t fa[2], fb[2], more_a = 0x3F803F80u, more_b = 0x3F803F80u;
-            if constexpr (NV) {
-                fa[0] = nv_scale(ca); fa[1] = nv_scale(ca >> 8);
-                fb[0] = nv_scale(cb); fb[1] = nv_scale(cb >> 8);
+            wa += w_next;
+            wb += w_next;
+            codes += codes_next;
+            ahead.base += ahead.split;
+            if (ahead.base >= l.steps) enter(ahead.following(ctas));
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        in = in + STAGE == ring_end ? ring : in + STAGE;
+    }
+    // Its own copies of a warp's oldest step are there, the other lanes' too.
+    __device__ __forceinline__ void await() const {
+        if (a.stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+    }
+
+    // x into its columns: 16 threads for the 128 elements of a token that share a scale.  Whether all of it is exact in FP16.
+    static constexpr int BATCH = T == EF_F32 ? 2 : 4;
+    struct Eights {
+        Raw<T> raw[BATCH];
+        int tok, o;                                     // of the first, the others 512 eights apart
+    };
+    __device__ __forceinline__ void ask(Eights& e) const {
+        const int token_eights = l.steps * (STEP / 8);
+        while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
+        int tok = e.tok, o = e.o;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            while (o >= token_eights) { o -= token_eights; ++tok; }
+            const bool there = tok < a.tokens && o * 8 < a.K;
+            e.raw[i] = load8<T, false>(static_cast<const E*>(a.x) + (there ? tok * a.ldx + o * 8 : 0), there ? 8 : 0, a.vec_x);
+            o += WARPS * 32;
+        }
+    }
+    __device__ __forceinline__ bool stage(Eights& e) {
+        const int token_eights = l.steps * (STEP / 8);
+        bool exact = true;
+        while (true) {
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
+                if (__any_sync(0xFFFFFFFFu, e.tok < a.tokens)) {
+                    const int half = e.o >> 4;
+                    unsigned char* at = smem + e.tok * P * l.pitch + block_at(half, e.o >> 2 & 3) + (e.o & 3) * 16;
+                    float* scale = (e.o & 15) == 0 ? reinterpret_cast<float*>(smem + l.scales) + half * NT * 8 + e.tok * P : nullptr;
+                    if (!stage_x<T>(e.raw[i], e.tok < a.tokens, at, l.pitch, scale) && e.tok < a.tokens) {
+                        exact = false;
+                        smem[l.flags + half / (STEP / HALF)] = 1;
+                    }
+                }
+                e.o += WARPS * 32;
+            }
+            while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
+            if (!__any_sync(0xFFFFFFFFu, e.tok < a.tokens)) break;
+            ask(e);
+        }
+        return exact;
+    }
+
+    // The tile's shares of its warps, put together.
+    __device__ __forceinline__ void finish(const Walk& now, float (&acc)[NT][4]) const {
+        constexpr int COLUMNS = BLOCKS ? NT * 2 : NT * 8;               // of a share
+        float* const share = reinterpret_cast<float*>(smem + l.share);
+        const int split = now.split, group = warp / split, bar = WARPS / split + group;         // barriers 1; 2, 3; 4 .. 7; 8 .. 15
+        const int first = threadIdx.x - group * split * 32;
+        float scale = 1.0f;
+        if (a.row_scale && first < ROWS * a.tokens && now.tile < tiles) scale = a.row_scale[min(now.tile * ROWS + (first & (ROWS - 1)), a.N - 1)];      // (the row is the same every time)
+        float* mine = share + warp * (ROWS * COLUMNS);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if constexpr (BLOCKS) {                     // the four columns of a token are in two lanes
+                float lo = __fadd_rn(acc[nt][0], acc[nt][1]), hi = __fadd_rn(acc[nt][2], acc[nt][3]);
+                lo = __fadd_rn(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, 1));
+                hi = __fadd_rn(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, 1));
+                if (!(t & 1)) {
+                    mine[g * COLUMNS + nt * 2 + (t >> 1)] = lo;
+                    mine[(g + 8) * COLUMNS + nt * 2 + (t >> 1)] = hi;
+                }
             } else {
-                mx_scale(ca, fa[0], more_a);
-                mx_scale(cb, fb[0], more_b);
-                fa[1] = fa[0]; fb[1] = fb[0];
+                *reinterpret_cast<float2*>(mine + g * COLUMNS + nt * 8 + 2 * t) = make_float2(acc[nt][0], acc[nt][1]);
+                *reinterpret_cast<float2*>(mine + (g + 8) * COLUMNS + nt * 8 + 2 * t) = make_float2(acc[nt][2], acc[nt][3]);
             }
-            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
+        }
+        asm volatile("bar.sync %0, %1;" :: "r"(bar), "r"(split * 32) : "memory");
+        if (now.tile < tiles) {
+            const float* shares = share + group * split * (ROWS * COLUMNS);
+            for (int o = first; o < ROWS * a.tokens; o += split * 32) {
+                const int r = o & (ROWS - 1), tok = o / ROWS, n = now.tile * ROWS + r;
+                float v = 0.0f;
 #pragma unroll
-            for (int word = 0; word < 4; ++word) {
-                uint4 b = make_uint4(0, 0, 0, 0);
-                if (g < columns) b = *reinterpret_cast<const uint4*>(xs + g * pitch + q * 64 + ((word + q + g) & 3) * 16);
-                uint32_t wr[4], ws[4];
-                decode(word == 0 ? va.x : word == 1 ? va.y : word == 2 ? va.z : va.w, wr);
-                decode(word == 0 ? vb.x : word == 1 ? vb.y : word == 2 ? vb.z : vb.w, ws);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    wr[j] = mul2(wr[j], fa[word / 2]);
-                    ws[j] = mul2(ws[j], fb[word / 2]);
-                    if constexpr (!NV) { wr[j] = mul2(wr[j], more_a); ws[j] = mul2(ws[j], more_b); }
+                for (int q = P - 1; q >= 0; --q) {      // the small parts first
+                    const float* at = shares + r * COLUMNS + tok * P + q;
+                    float s = 0.0f;
+                    for (int w = 0; w < split; w += 2) s = __fadd_rn(s, __fadd_rn(at[w * (ROWS * COLUMNS)], at[(w + 1) * (ROWS * COLUMNS)]));
+                    v = __fadd_rn(v, s);
                 }
-                mma(d, wr[0], ws[0], wr[1], ws[1], b.x, b.y);
-                mma(d, wr[2], ws[2], wr[3], ws[3], b.z, b.w);
+                if (n < a.N) {
+                    v = __fmul_rn(v, scale);
+                    E* y = static_cast<E*>(a.y) + tok * a.ldy + n;
+                    if constexpr (T == EF_F32) *y = v;
+                    else if constexpr (T == EF_BF16) *y = __float2bfloat16_rn(v);
+                    else *y = __float2half_rn(v);
+                }
             }
+        }
+        asm volatile("bar.sync %0, %1;" :: "r"(bar), "r"(split * 32) : "memory");
+    }
+
+    // GENERAL: of any K, codes from memory where they are not copied, steps that are not exact in FP16.
+    template <bool GENERAL> __device__ __forceinline__ void run() {
+        std::conditional_t<BLOCKS, BlockProduct<NV, NT>, Product<NV, NT>> product;
+        Walk now;
+        now.begin(0, tiles, ctas);
+        product.begin(l, a.tokens * P, lane, now.step(), now.split);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = __fadd_rn(acc[i], d[i]);
+        for (int nt = 0; nt < NT; ++nt) product.acc[nt][0] = product.acc[nt][1] = product.acc[nt][2] = product.acc[nt][3] = 0.0f;
+        while (now.done < tiles) {
+            fetch<GENERAL>();
+            await();
+            const int step = now.step();
+            if (now.tile < tiles && step < l.steps) {
+                const uint32_t at = out + lane * 16;
+                const uint4 va[2] = {load16(at), load16(at + 512)}, vb[2] = {load16(at + 1024), load16(at + 1536)};
+                // the codes of the blocks that the lane decodes (half, row), or that its sums are of
+                const bool wide = GENERAL && T != EF_F16 && smem[l.flags + step], by_block = BLOCKS && !wide;
+                uint32_t codes[2][2];
+                const int block = by_block ? (t & 1) * 2 : t;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if (!GENERAL || a.copy_codes) {
+                            const uint8_t* from = smem + out + 2048 + g * ROW_CODES + block * CODES + r * (8 * ROW_CODES) + h * (4 * CODES);
+                            codes[h][r] = by_block ? load_codes<NV>(from) : load_code<NV>(from);
+                        } else {
+                            const uint8_t* from = a.sf + int64_t(min(now.tile * ROWS + g + r * 8, a.N - 1)) * (chunks * CODES);
+                            const int q = step * 8 + 4 * h + block;
+                            codes[h][r] = load_code<NV>(from + min(q, chunks - 1) * CODES);
+                            if (by_block) codes[h][r] |= load_code<NV>(from + min(q + 1, chunks - 1) * CODES) << 16;
+                        }
+                    }
+                if (wide) {
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const int k = step * STEP + h * HALF + t * 32;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            product.add(nt, wide_sums<T, NV>(h ? va[1] : va[0], h ? vb[1] : vb[0], h ? codes[1][0] : codes[0][0], h ? codes[1][1] : codes[0][1], static_cast<const E*>(a.x), a.ldx,
+                                                             a.vec_x, a.tokens * PER_TOKEN, PER_TOKEN, nt * 8, k < a.K ? k : -1));
+                    }
+                } else if constexpr (BLOCKS) product.step(va, vb, codes);
+                else {
+                    const Item it[2] = {{va[0], vb[0], codes[0][0], codes[0][1]}, {va[1], vb[1], codes[1][0], codes[1][1]}};
+                    if constexpr (NV) product.step_nv(it);
+                    else product.step_mx(it);
+                }
+            }
+            out = out + STAGE == ring_end ? ring : out + STAGE;
+            now.base += now.split;
+            product.next();
+            if (now.base < l.steps) continue;
+            finish(now, product.acc);
+            now.begin(now.following(ctas), tiles, ctas);
+            product.begin(l, a.tokens * P, lane, now.step(), now.split);
         }
     }
-    share[warp][g][2 * t] = acc[0];
-    share[warp][g][2 * t + 1] = acc[1];
-    share[warp][g + 8][2 * t] = acc[2];
-    share[warp][g + 8][2 * t + 1] = acc[3];
+};
+
+// BLOCKS: of BlockProduct, a token has four columns of the instruction but one in shared memory.
+template <int T, bool NV, int NT, bool BLOCKS>
+__global__ void __launch_bounds__(WARPS * 32, 1) matvec4_kernel(const MatvecArgs a) {
+    after_previous();
+    Kernel<T, NV, NT, BLOCKS> k(a);
+    // x is asked for before the weights' stream begins, and staged before more than a step a warp of it is in front.
+    typename Kernel<T, NV, NT, BLOCKS>::Eights eights;
+    eights.tok = 0;
+    eights.o = threadIdx.x;
+    k.ask(eights);
+    const bool plain = a.K % STEP == 0 && a.copy_codes;
+    if (plain) k.template fetch<false>();
+    else k.template fetch<true>();
+    const Layout& l = k.l;
+    for (int i = threadIdx.x; i < l.steps; i += WARPS * 32) smem[l.flags + i] = 0;
+    for (int i = threadIdx.x; i < 2 * HALF_BYTES / 4; i += WARPS * 32) reinterpret_cast<uint32_t*>(smem + l.zeros)[i] = 0u;
+    for (int i = threadIdx.x; i < l.steps * (STEP / HALF) * NT * 8; i += WARPS * 32) reinterpret_cast<float*>(smem + l.scales)[i] = 0.0f;
     __syncthreads();
-    for (int i = threadIdx.x; i < ROWS * a.tokens; i += WARPS * 32) {
-        const int r = i % ROWS, tok = i / ROWS, n = blockIdx.x * ROWS + r;
-        if (n >= a.N) continue;
-        float v = 0.0f;
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) {          // the small parts first
-            float s = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) s = __fadd_rn(s, share[w][r][tok * PARTS + p]);
-            v = __fadd_rn(v, s);
-        }
-        if constexpr (NV) v = __fmul_rn(v, 256.0f);
-        if (a.row_scale) v = __fmul_rn(v, a.row_scale[n]);
-        E* y = static_cast<E*>(a.y) + tok * a.ldy + n;
-        if constexpr (T == EF_F32) *y = v;
-        else if constexpr (T == EF_BF16) *y = __float2bfloat16_rn(v);
-        else *y = __float2half_rn(v);
+    const bool wide = __syncthreads_or(!k.stage(eights));
+    for (int i = 2; i < a.stages; ++i) {
+        if (plain) k.template fetch<false>();
+        else k.template fetch<true>();
     }
+    if (plain && !wide) k.template run<false>();
+    else k.template run<true>();
 }
 
+template <int T, bool NV, int NT, bool BLOCKS>
+cudaError_t launch(const MatvecArgs& a, size_t smem, cudaStream_t stream) {
+    if (smem > 48 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(matvec4_kernel<T, NV, NT, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(SMEM_MOST));
+        if (err != cudaSuccess) { cudaGetLastError(); return err; }
+    }
+    const int tiles = (a.N + ROWS - 1) / ROWS;
+    return enqueue(matvec4_kernel<T, NV, NT, BLOCKS>, dim3(unsigned(tiles < 148 ? tiles : 148)), WARPS * 32, smem, stream, a);
+}
 template <int T, bool NV>
-cudaError_t launch(MatvecArgs a, int64_t T_all, int64_t bytes, cudaStream_t stream) {
-    constexpr int PARTS = T == EF_BF16 ? 1 : (T == EF_F16 ? 2 : 3), MOST = 8 / PARTS;
+cudaError_t launch(MatvecArgs a, int64_t all, int64_t bytes, cudaStream_t stream) {
+    // tokens that read the weights together: 16 columns, as many as shared memory holds beside the shortest ring
+    int most = 16 / PARTS<T>;
+    while (layout(a.K, most * PARTS<T>, most * PARTS<T> > 8 ? 2 : 1, 2).end > SMEM_MOST) --most;
     const char *x = static_cast<const char*>(a.x), *y = static_cast<const char*>(a.y);
     cudaError_t err = cudaSuccess;
-    for (int64_t done = 0; done < T_all && err == cudaSuccess; done += MOST) {
-        a.tokens = int(T_all - done < MOST ? T_all - done : MOST);
+    most = int((all + (all + most - 1) / most - 1) / ((all + most - 1) / most));       // evenly
+    for (int64_t done = 0; done < all && err == cudaSuccess; done += a.tokens) {
+        a.tokens = int(all - done < most ? all - done : most);
         a.x = x + done * a.ldx * bytes;
         a.y = const_cast<char*>(y) + done * a.ldy * bytes;
-        const int columns = a.tokens * PARTS;
-        a.slice = SMEM_X / (64 * columns) / 4 * 4;
-        if (a.slice > (a.K / 32 + 3) / 4 * 4) a.slice = (a.K / 32 + 3) / 4 * 4;
-        err = enqueue(matvec4_kernel<T, NV>, dim3(unsigned((a.N + ROWS - 1) / ROWS)), WARPS * 32, size_t(columns) * a.slice * 64, stream, a);
+        const int columns = a.tokens * PARTS<T>;
+        const bool blocks = PARTS<T> == 1 && a.tokens <= BLOCK_TOKENS;
+        const int nt = blocks ? (a.tokens <= 2 ? 1 : 2) : (columns <= 8 ? 1 : 2);
+        a.stages = layout(a.K, columns, nt, 4).end <= SMEM_MOST ? 4 : 2;
+        const size_t smem = layout(a.K, columns, nt, a.stages).end;
+        if constexpr (PARTS<T> == 1) {
+            if (blocks) { err = nt == 1 ? launch<T, NV, 1, true>(a, smem, stream) : launch<T, NV, 2, true>(a, smem, stream); continue; }
+        }
+        err = nt == 1 ? launch<T, NV, 1, false>(a, smem, stream) : launch<T, NV, 2, false>(a, smem, stream);
     }
     return err;
 }
@@ -204,6 +765,7 @@ int launch_matvec4(bool nv, int fmt, int64_t T, int64_t N, int64_t K, const void
     a.row_scale = row_scale;
     a.x = x; a.y = y;
     a.ldw = ldw / 2; a.ldx = ldx; a.ldy = ldy;
+    a.copy_codes = K % STEP == 0 && reinterpret_cast<uintptr_t>(sf) % (nv ? 16 : 8) == 0;
     a.vec_x = (reinterpret_cast<uintptr_t>(x) | uintptr_t(ldx * bytes)) % 16 == 0;
     const cudaError_t err = fmt == EF_F32 ? launch<EF_F32>(nv, a, T, bytes, stream) : fmt == EF_BF16 ? launch<EF_BF16>(nv, a, T, bytes, stream) : launch<EF_F16>(nv, a, T, bytes, stream);
     if (err != cudaSuccess) { set_error("mmasim_matvec4: %s", cudaGetErrorString(err)); return MMASIM_ERR_CUDA; }

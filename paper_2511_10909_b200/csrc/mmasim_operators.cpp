@@ -212,8 +212,8 @@ int mmasim_matvec4(int w_fmt, int fmt, int64_t T, int64_t N, int64_t K, const vo
     const char* call = "mmasim_matvec4";
     if (!packed4(w_fmt)) { set_error("%s: weights are MXF4_GST or NVF4_GST", call); return MMASIM_ERR_UNSUPPORTED; }
     if (element_fmt(fmt) < 0) { set_error("%s: x and y are FP32, BF16 or FP16", call); return MMASIM_ERR_INVALID_ARG; }
-    if (T < 0 || T > 0x7FFFFFFF || N < 1 || N > 0x7FFFFFF0 || K < 32 || K % 32 || K > 0x7FFFFFE0) {
-        set_error("%s: T = %lld, N = %lld, K = %lld: T >= 0, N >= 1 and K a multiple of 32 are taken, below 2^31", call, (long long)T, (long long)N, (long long)K);
+    if (T < 0 || T > 0x7FFFFFFF || N < 1 || N > 0x40000000 || K < 32 || K % 32 || K > (fmt == MMASIM_F32 ? MATVEC_MAX_K_F32 : ROWS_MAX_K)) {
+        set_error("%s: T = %lld, N = %lld, K = %lld: T from 0 on, N from 1 to 2^30 and multiples of 32 up to 32768 (FP32: 28672) for K are taken", call, (long long)T, (long long)N, (long long)K);
         return MMASIM_ERR_SHAPE;
     }
     int st = check_ld(call, "W", &ldw, K);

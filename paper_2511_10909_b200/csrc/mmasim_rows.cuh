@@ -28,38 +28,40 @@ struct Args {
     uint8_t* sf;
     float* row_scale;
     int64_t ldx, ldr, ldh, ldo, ld_sf;      // in elements (FP4: two per byte)
-    float eps;
+    float eps, inverse_k;
     int e5m2;                               // FP8: which
     int w_f32;
     int vec_x, vec_r, vec_h, vec_o, vec_w;  // every row starts where eight elements can be moved at once
 };
 
-// Sum, or largest, of the row's threads; `slot`: 16 words of shared memory that nothing else uses.
+// Sum, or largest, of the row's threads, for all of them; `slot`: 16 words of shared memory that nothing else uses.
 __device__ __forceinline__ float row_sum(float v, int threads, float* slot) {
     for (int o = min(threads, 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     if (threads > 32) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = int(threadIdx.x & 31) < threads / 32 ? slot[threadIdx.x & 31] : 0.0f;
+        v = int(threadIdx.x & 15) < threads / 32 ? slot[threadIdx.x & 15] : 0.0f;
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     }
-    return __shfl_sync(0xFFFFFFFFu, v, threads > 32 ? 0 : (threadIdx.x & 31) & ~(threads - 1));
+    return v;
 }
 __device__ __forceinline__ uint32_t row_max(uint32_t v, int threads, uint32_t* slot) {
-    for (int o = min(threads, 32) / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    if (threads < 32) {
+        for (int o = threads / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+        return v;
+    }
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
     if (threads > 32) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = int(threadIdx.x & 31) < threads / 32 ? slot[threadIdx.x & 31] : 0u;
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-        v = __shfl_sync(0xFFFFFFFFu, v, 0);
+        v = __reduce_max_sync(0xFFFFFFFFu, int(threadIdx.x & 31) < threads / 32 ? slot[threadIdx.x & 31] : 0u);
     }
     return v;
 }
 
-template <int T, int OUT, int V, bool NORM>
+// VEC: rows of whole eights, all of which start on 16 bytes (codes: on their eight or four).
+template <int T, int OUT, int V, bool NORM, bool VEC>
 __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
     using namespace quant;
     using E = typename Elem<T>::type;
@@ -69,155 +71,187 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int64_t row = int64_t(blockIdx.x) * per_cta + (a.threads > 32 ? 0 : threadIdx.x / a.threads);
     const int t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
-    const bool live = row < a.M;            // (the others of the last CTA take part in the exchanges between lanes)
+    // NVF4: two eights side by side where a thread has several, one scale for both (BF16 4096 x 4096: 13.4 us without, 10.9 with; FP32 rows
+    // read 64 bytes a thread that way, and a norm of 4096 x 4096 took 47 us, not 37)
+    constexpr int SIDE = OUT == OUT_NVF4 && V > 1 && T != EF_F32 ? 2 : 1;
+    auto place = [&](int j) { return (t + j / SIDE * a.threads) * (8 * SIDE) + j % SIDE * 8; };
+    const int K = row < a.M ? a.K : 0;      // (threads of the last CTA without a row take part in the exchanges between lanes)
     const E* x = static_cast<const E*>(a.x) + row * a.ldx;
 
-    float y[V][8];
-    int n[V];                               // elements of this eight within the row
+    Raw<T> h[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        n[j] = live ? a.K - (t + j * a.threads) * 8 : 0;
-        widen<T>(load8<T>(x + (n[j] > 0 ? (t + j * a.threads) * 8 : 0), n[j], a.vec_x), y[j]);
-    }
+    for (int j = 0; j < V; ++j) h[j] = load8<T, VEC>(x + place(j), K - place(j), a.vec_x);
+    Pair y[NORM ? V : 1][4];                // without a norm the elements stay as they were loaded until their codes are made
     if constexpr (NORM) {
         if (a.residual) {
             const E* r = static_cast<const E*>(a.residual) + row * a.ldr;
+            E* out = static_cast<E*>(a.h_out) + row * a.ldh;
             Raw<T> res[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) res[j] = load8<T>(r + (n[j] > 0 ? (t + j * a.threads) * 8 : 0), n[j], a.vec_r);
+            for (int j = 0; j < V; ++j) res[j] = load8<T, VEC>(r + place(j), K - place(j), a.vec_r);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float v[8];
-                widen<T>(res[j], v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[j][i] = __fadd_rn(y[j][i], v[i]);
-                Raw<T> h;
-                narrow<T>(y[j], h);
-                widen<T>(h, y[j]);          // the norm is taken of what is stored: the backward pass has nothing else
-                if (n[j] > 0) store8<T>(static_cast<E*>(a.h_out) + row * a.ldh + (t + j * a.threads) * 8, h, n[j], a.vec_h);
+            for (int j = 0; j < V; ++j) {   // the norm is taken of what is stored: the backward pass has nothing else
+                add_to<T>(h[j], res[j]);
+                if (place(j) < K) store8<T, VEC>(out + place(j), h[j], K - place(j), a.vec_h);
             }
         }
-        float sum = 0.0f;
+        constexpr bool EARLY = V <= 2;      // asked for before the row's threads wait for one another, where the registers hold them
+        Pair w[EARLY ? V : 1][4];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = __fmaf_rn(y[j][i], y[j][i], sum);
-        const float r = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(sum, a.threads, sum_slot), float(a.K)), a.eps));
+        for (int j = 0; j < V && EARLY; ++j) load_weight8<T, VEC>(a.w, a.w_f32, place(j), K - place(j), a.vec_w, w[j]);
+        Pair squares = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            float w[8];
-            load_weight8<T>(a.w, a.w_f32, n[j] > 0 ? (t + j * a.threads) * 8 : 0, n[j], a.vec_w, w);
+            widen<T>(h[j], y[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[j][i] = i < n[j] ? __fmul_rn(__fmul_rn(y[j][i], r), w[i]) : 0.0f;
+            for (int i = 0; i < 4; ++i) squares = fma2(y[j][i], y[j][i], squares);
+        }
+        float even, odd;
+        split(squares, even, odd);
+        const Pair r = both(inverse_root(__fmaf_rn(row_sum(even + odd, a.threads, sum_slot), a.inverse_k, a.eps)));
+        // (behind the row's end: zeros times zeros, and where r is not finite no element of the row is a number)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if constexpr (!EARLY) load_weight8<T, VEC>(a.w, a.w_f32, place(j), K - place(j), a.vec_w, w[0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[j][i] = mul2(mul2(y[j][i], r), w[EARLY ? j : 0][i]);
         }
     }
 
     if constexpr (OUT == OUT_PLAIN) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (n[j] > 0) {
-                Raw<T> o;
-                narrow<T>(y[j], o);
-                store8<T>(static_cast<E*>(a.out) + row * a.ldo + (t + j * a.threads) * 8, o, n[j], a.vec_o);
-            }
+        for (int j = 0; j < V; ++j) {
+            const int at = place(j);
+            Raw<T> o;
+            narrow<T>(y[j], o);
+            if (at < K) store8<T, VEC>(static_cast<E*>(a.out) + row * a.ldo + at, o, K - at, a.vec_o);
+        }
         return;
     }
-    float scale = 0.0f;                     // of the row
-    uint32_t amax[V];                       // of this eight, then of its block
-#pragma unroll
-    for (int j = 0; j < V; ++j) amax[j] = magnitude_bits(y[j]);
+    float scale = 0.0f, unit = 0.0f;        // of the row; NVF4: six times the scale
     if constexpr (OUT == OUT_FP8 || OUT == OUT_NVF4) {
         uint32_t top = 0u;
 #pragma unroll
-        for (int j = 0; j < V; ++j) top = max(top, amax[j]);
+        for (int j = 0; j < V; ++j) {
+            if constexpr (NORM) top = largest(top, y[j]);
+            else largest_halves<T>(top, h[j]);
+        }
+        if constexpr (!NORM) top = largest_of<T>(top);
         top = row_max(top, a.threads, max_slot);
         if (top >= INF_BITS) scale = __uint_as_float(0x7FC00000u);
         else if constexpr (OUT == OUT_NVF4) scale = fmaxf(__fdiv_rn(__uint_as_float(top), 2688.0f), 7.88860905e-31f);       // 2^-100: g times it stays normal
         else scale = fmaxf(__fdiv_rn(__uint_as_float(top), a.e5m2 ? 57344.0f : 448.0f), 1.17549435e-38f);                    // 2^-126
-        if (t == 0 && live) a.row_scale[row] = scale;
+        unit = __fmul_rn(6.0f, scale);
+        if (t == 0 && K > 0) a.row_scale[row] = scale;
     }
-    if constexpr (OUT == OUT_FP8) {
-        const Divisor by(scale);
+    const Divisor by(OUT == OUT_NVF4 ? unit : scale);
 #pragma unroll
-        for (int j = 0; j < V; ++j) by.apply(y[j]);
-    }
+    for (int j0 = 0; j0 < V; j0 += SIDE) {
+        const int at = place(j0);
+        Pair v[SIDE][4];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int at = (t + j * a.threads) * 8;
+        for (int k = 0; k < SIDE; ++k) {
+            if constexpr (!NORM) widen<T>(h[j0 + k], v[k]);
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[k][i] = y[j0 + k][i];
+            }
+        }
         bool zero = false;                  // FP4 has no code for a block without numbers
+        if constexpr (OUT == OUT_FP8) by.apply(v[0]);
         if constexpr (OUT == OUT_MX8 || OUT == OUT_MXF4) {
-            amax[j] = max(amax[j], __shfl_xor_sync(0xFFFFFFFFu, amax[j], 1));
-            amax[j] = max(amax[j], __shfl_xor_sync(0xFFFFFFFFu, amax[j], 2));
-            const uint32_t code = e8m0_code(amax[j], OUT == OUT_MXF4 ? 2 : (a.e5m2 ? 15 : 8));
-            const float f = e8m0_inverse(code);
+            uint32_t top = largest(0u, v[0]);
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const uint32_t code = e8m0_code(top, OUT == OUT_MXF4 ? 2 : (a.e5m2 ? 15 : 8));
+            const Pair f = both(e8m0_inverse(code));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[j][i] = __fmul_rn(y[j][i], f);
+            for (int i = 0; i < 4; ++i) v[0][i] = mul2(v[0][i], f);
             zero = code == 255u;
-            if ((t & 3) == 0 && n[j] > 0) a.sf[row * a.ld_sf + at / 32] = uint8_t(code);
+            if ((t & 3) == 0 && at < K) a.sf[row * a.ld_sf + at / 32] = uint8_t(code);
         }
         if constexpr (OUT == OUT_NVF4) {
-            amax[j] = max(amax[j], __shfl_xor_sync(0xFFFFFFFFu, amax[j], 1));
-            const uint32_t code = scale == scale ? ue4m3_code(__fdiv_rn(__uint_as_float(amax[j]), __fmul_rn(6.0f, scale))) : 0x7Fu;
-            Divisor(__fmul_rn(ue4m3_value(code), scale)).apply(y[j]);
+            uint32_t top = largest(0u, v[0]);
+            if constexpr (SIDE == 2) top = largest(top, v[1]);
+            else top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            const uint32_t code = scale == scale ? ue4m3_code(by(__uint_as_float(top))) : 0x7Fu;
+            const Divisor of(__fmul_rn(ue4m3_value(code), scale));
+#pragma unroll
+            for (int k = 0; k < SIDE; ++k) of.apply(v[k]);
             zero = code == 0x7Fu;
-            if ((t & 1) == 0 && n[j] > 0) a.sf[row * a.ld_sf + at / 16] = uint8_t(code);
+            if ((SIDE == 2 || (t & 1) == 0) && at < K) a.sf[row * a.ld_sf + at / 16] = uint8_t(code);
         }
-        if (n[j] <= 0) continue;
+        if (at >= K) continue;
         if constexpr (OUT == OUT_FP8 || OUT == OUT_MX8) {
-            const uint2 c = a.e5m2 ? codes_e5m2(y[j]) : codes_e4m3(y[j]);
+            const uint2 c = a.e5m2 ? codes_e5m2(v[0]) : codes_e4m3(v[0]);
             uint8_t* p = static_cast<uint8_t*>(a.out) + row * a.ldo + at;
-            if (a.vec_o && n[j] >= 8) *reinterpret_cast<uint2*>(p) = c;
+            if (VEC || (a.vec_o && at + 8 <= K)) *reinterpret_cast<uint2*>(p) = c;
             else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (i < n[j]) p[i] = uint8_t((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+                for (int i = 0; i < 8; ++i) if (at + i < K) p[i] = uint8_t((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
             }
         } else {
-            const uint32_t c = zero ? 0u : codes_e2m1(y[j]);
             uint8_t* p = static_cast<uint8_t*>(a.out) + (row * a.ldo + at) / 2;
-            if (a.vec_o) *reinterpret_cast<uint32_t*>(p) = c;                // (K is a multiple of 32)
-            else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = uint8_t(c >> (8 * i));
+            for (int k = 0; k < SIDE; ++k, p += 4) {
+                const uint32_t c = zero ? 0u : codes_e2m1(v[k]);
+                if (VEC || a.vec_o) *reinterpret_cast<uint32_t*>(p) = c;     // (K is a multiple of 32)
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = uint8_t(c >> (8 * i));
+                }
             }
         }
     }
 }
 
-// Threads per row and eights per thread.
+// Threads per row and eights per thread.  Few rows are a matter of latency: the most threads.  Many rows are one of instructions, and what a
+// thread does once a row (the exchanges, the scale) counts less with several eights: a norm takes 256 threads, where its rows need more than
+// four eights of them the fewest that do, quantisation 128.  BF16, 4096 x 4096, us with 512 / 256 / 128 threads: norm into MXFP8 23.5 / 21.1 /
+// 22.2, E4M3 rows 13.7 / 11.0 / 9.9; norm of 16384 x 8192 into E4M3 with 512 / 256 threads 170 / 138.
+constexpr int64_t FEW_ROWS = 296;
 struct Shape { int threads, v; };
-inline Shape shape(int64_t M, int K) {
+inline Shape shape(int64_t M, int K, bool norm) {
     const int eights = (K + 7) / 8;
     if (eights <= 8) return {8, 1};
     if (eights <= 16) return {16, 1};
     if (eights <= 32) return {32, 1};
     int v = 1;
+    while (M > FEW_ROWS && v < 4 && eights > v * (norm ? 256 : 128)) v *= 2;
     while (eights > v * MAX_THREADS) v *= 2;
-    (void)M;
     return {((eights + v - 1) / v + 31) / 32 * 32, v};
 }
 
-template <int T, int OUT, bool NORM>
+template <int T, int OUT, bool NORM, bool VEC>
 cudaError_t launch_out(const Args& a, int v, cudaStream_t stream) {
     const unsigned block = a.threads > 32 ? unsigned(a.threads) : 128u;
     const int per_cta = a.threads > 32 ? 1 : 128 / a.threads;
     const dim3 grid(unsigned((a.M + per_cta - 1) / per_cta));
     switch (v) {
-        case 1: return enqueue(rows_kernel<T, OUT, 1, NORM>, grid, block, 0, stream, a);
-        case 2: return enqueue(rows_kernel<T, OUT, 2, NORM>, grid, block, 0, stream, a);
-        case 4: return enqueue(rows_kernel<T, OUT, 4, NORM>, grid, block, 0, stream, a);
-        default: return enqueue(rows_kernel<T, OUT, 8, NORM>, grid, block, 0, stream, a);
+        case 1: return enqueue(rows_kernel<T, OUT, 1, NORM, VEC>, grid, block, 0, stream, a);
+        case 2: return enqueue(rows_kernel<T, OUT, 2, NORM, VEC>, grid, block, 0, stream, a);
+        case 4: return enqueue(rows_kernel<T, OUT, 4, NORM, VEC>, grid, block, 0, stream, a);
+        default: return enqueue(rows_kernel<T, OUT, 8, NORM, VEC>, grid, block, 0, stream, a);
     }
+}
+template <int T, int OUT>
+cudaError_t launch_out(const Args& a, int v, bool norm, cudaStream_t stream) {
+    const bool vec = a.K % 8 == 0 && a.vec_x && a.vec_o && a.vec_w && (!a.residual || (a.vec_r && a.vec_h));
+    if constexpr (OUT != OUT_PLAIN)
+        if (!norm) return vec ? launch_out<T, OUT, false, true>(a, v, stream) : launch_out<T, OUT, false, false>(a, v, stream);
+    return vec ? launch_out<T, OUT, true, true>(a, v, stream) : launch_out<T, OUT, true, false>(a, v, stream);
 }
 template <int T>
 cudaError_t launch_type(Args a, int out, bool norm, cudaStream_t stream) {
-    const Shape s = shape(a.M, a.K);
+    const Shape s = shape(a.M, a.K, norm);
     a.threads = s.threads;
+    a.inverse_k = 1.0f / float(a.K);
     switch (out) {
-        case OUT_PLAIN: return launch_out<T, OUT_PLAIN, true>(a, s.v, stream);
-        case OUT_FP8: return norm ? launch_out<T, OUT_FP8, true>(a, s.v, stream) : launch_out<T, OUT_FP8, false>(a, s.v, stream);
-        case OUT_MX8: return norm ? launch_out<T, OUT_MX8, true>(a, s.v, stream) : launch_out<T, OUT_MX8, false>(a, s.v, stream);
-        case OUT_MXF4: return norm ? launch_out<T, OUT_MXF4, true>(a, s.v, stream) : launch_out<T, OUT_MXF4, false>(a, s.v, stream);
-        default: return norm ? launch_out<T, OUT_NVF4, true>(a, s.v, stream) : launch_out<T, OUT_NVF4, false>(a, s.v, stream);
+        case OUT_PLAIN: return launch_out<T, OUT_PLAIN>(a, s.v, norm, stream);
+        case OUT_FP8: return launch_out<T, OUT_FP8>(a, s.v, norm, stream);
+        case OUT_MX8: return launch_out<T, OUT_MX8>(a, s.v, norm, stream);
+        case OUT_MXF4: return launch_out<T, OUT_MXF4>(a, s.v, norm, stream);
+        default: return launch_out<T, OUT_NVF4>(a, s.v, norm, stream);
     }
 }
 

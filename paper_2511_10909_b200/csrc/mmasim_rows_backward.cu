@@ -21,7 +21,7 @@ struct BackArgs {
     void* dx;
     float* part;                            // gridDim.x rows of K, or NULL
     int64_t ld_dy, ld_h, ld_res, ld_dx;
-    float eps;
+    float eps, inverse_k;
     int w_f32, vec_dy, vec_h, vec_res, vec_dx, vec_w;
 };
 
@@ -33,19 +33,18 @@ __device__ __forceinline__ float2 row_sums(float2 v, int threads, float2* slot) 
     if (threads > 32) {
         if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = int(threadIdx.x & 31) < threads / 32 ? slot[threadIdx.x & 31] : make_float2(0.0f, 0.0f);
+        v = int(threadIdx.x & 15) < threads / 32 ? slot[threadIdx.x & 15] : make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) {
             v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
             v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
         }
     }
-    const int from = threads > 32 ? 0 : (threadIdx.x & 31) & ~(threads - 1);
-    return make_float2(__shfl_sync(0xFFFFFFFFu, v.x, from), __shfl_sync(0xFFFFFFFFu, v.y, from));
+    return v;
 }
 
 // HOLD: dy and h stay in registers between the sums and the results; else they are read again (rows too long for that).
-template <int T, int V, bool HOLD>
+template <int T, int V, bool HOLD, bool VEC>
 __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a) {
     using E = typename Elem<T>::type;
     __shared__ float2 slots[2][16];
@@ -53,75 +52,84 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
-    float dw[V][8];
+    Pair dw[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) dw[j][i] = 0;
     int turn = 0;
     for (int64_t first = int64_t(blockIdx.x) * per_cta; first < a.M; first += int64_t(gridDim.x) * per_cta, turn ^= 1) {
         const int64_t row = first + group;
+        const int K = row < a.M ? a.K : 0;
         const E *dy = static_cast<const E*>(a.dy) + row * a.ld_dy, *h = static_cast<const E*>(a.h) + row * a.ld_h;
-        Raw<T> dy_raw[HOLD ? V : 1], h_raw[HOLD ? V : 1];
-        float2 sums = make_float2(0.0f, 0.0f);
+        Raw<T> dy_raw[HOLD ? V : 1], h_raw[HOLD ? V : 1], res_raw[HOLD ? V : 1];
         if constexpr (HOLD) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int at = (t + j * a.threads) * 8, n = row < a.M ? a.K - at : 0;
-                h_raw[j] = load8<T>(h + (n > 0 ? at : 0), n, a.vec_h);
-                dy_raw[j] = load8<T>(dy + (n > 0 ? at : 0), n, a.vec_dy);
+                const int at = (t + j * a.threads) * 8;
+                h_raw[j] = load8<T, VEC>(h + at, K - at, a.vec_h);
+                dy_raw[j] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
+                if (a.dres) res_raw[j] = load8<T, VEC>(static_cast<const E*>(a.dres) + row * a.ld_res + at, K - at, a.vec_res);
             }
         }
+        Pair squares = 0, products = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int at = (t + j * a.threads) * 8, n = row < a.M ? a.K - at : 0;
+            const int at = (t + j * a.threads) * 8;
             if constexpr (!HOLD) {
-                h_raw[0] = load8<T>(h + (n > 0 ? at : 0), n, a.vec_h);
-                dy_raw[0] = load8<T>(dy + (n > 0 ? at : 0), n, a.vec_dy);
+                h_raw[0] = load8<T, VEC>(h + at, K - at, a.vec_h);
+                dy_raw[0] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
             }
-            float hv[8], g[8], w[8];
+            Pair hv[4], g[4], w[4];
             widen<T>(h_raw[HOLD ? j : 0], hv);
             widen<T>(dy_raw[HOLD ? j : 0], g);
-            load_weight8<T>(a.w, a.w_f32, n > 0 ? at : 0, n, a.vec_w, w);
+            load_weight8<T, VEC>(a.w, a.w_f32, at, K - at, a.vec_w, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sums.x = __fmaf_rn(hv[i], hv[i], sums.x);
-                sums.y = __fmaf_rn(__fmul_rn(g[i], w[i]), hv[i], sums.y);
+            for (int i = 0; i < 4; ++i) {
+                squares = fma2(hv[i], hv[i], squares);
+                products = fma2(mul2(g[i], w[i]), hv[i], products);
             }
         }
-        sums = row_sums(sums, a.threads, slots[turn]);          // (two sets of slots: one barrier a row)
-        const float r = __frsqrt_rn(__fadd_rn(__fdiv_rn(sums.x, float(a.K)), a.eps));
-        const float c = __fdiv_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), float(a.K));
+        float2 sums, odd;
+        split(squares, sums.x, odd.x);
+        split(products, sums.y, odd.y);
+        sums = row_sums(make_float2(sums.x + odd.x, sums.y + odd.y), a.threads, slots[turn]);          // (two sets of slots: one barrier a row)
+        const float r = inverse_root(__fmaf_rn(sums.x, a.inverse_k, a.eps));
+        const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int at = (t + j * a.threads) * 8, n = row < a.M ? a.K - at : 0;
-            if (n <= 0) continue;
+            const int at = (t + j * a.threads) * 8;
+            if (at >= K) continue;
             if constexpr (!HOLD) {
-                h_raw[0] = load8<T>(h + at, n, a.vec_h);
-                dy_raw[0] = load8<T>(dy + at, n, a.vec_dy);
+                h_raw[0] = load8<T, VEC>(h + at, K - at, a.vec_h);
+                dy_raw[0] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
+                if (a.dres) res_raw[0] = load8<T, VEC>(static_cast<const E*>(a.dres) + row * a.ld_res + at, K - at, a.vec_res);
             }
-            float hv[8], g[8], w[8], res[8];
+            Pair hv[4], g[4], w[4], out[4];
             widen<T>(h_raw[HOLD ? j : 0], hv);
             widen<T>(dy_raw[HOLD ? j : 0], g);
-            load_weight8<T>(a.w, a.w_f32, at, n, a.vec_w, w);
-            if (a.dres) widen<T>(load8<T>(static_cast<const E*>(a.dres) + row * a.ld_res + at, n, a.vec_res), res);
+            load_weight8<T, VEC>(a.w, a.w_f32, at, K - at, a.vec_w, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                dw[j][i] = __fmaf_rn(g[i], __fmul_rn(hv[i], r), dw[j][i]);
-                float v = __fmaf_rn(__fmul_rn(g[i], w[i]), r, -__fmul_rn(hv[i], c));
-                if (a.dres) v = __fadd_rn(v, res[i]);
-                hv[i] = v;
+            for (int i = 0; i < 4; ++i) {
+                dw[j][i] = fma2(g[i], mul2(hv[i], rr), dw[j][i]);
+                out[i] = fma2(mul2(g[i], w[i]), rr, mul2(hv[i], c));
+            }
+            if (a.dres) {
+                Pair res[4];
+                widen<T>(res_raw[HOLD ? j : 0], res);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = add2(out[i], res[i]);
             }
             Raw<T> o;
-            narrow<T>(hv, o);
-            store8<T>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, n, a.vec_dx);
+            narrow<T>(out, o);
+            store8<T, VEC>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, K - at, a.vec_dx);
         }
     }
     if (!a.part) return;
     float* mine = a.part + int64_t(blockIdx.x) * a.K;
     if (a.threads <= 32) {                  // (V = 1) several rows at a time: the groups' shares first
 #pragma unroll
-        for (int i = 0; i < 8; ++i) group_share[threadIdx.x * 8 + i] = dw[0][i];
+        for (int i = 0; i < 4; ++i) split(dw[0][i], group_share[threadIdx.x * 8 + 2 * i], group_share[threadIdx.x * 8 + 2 * i + 1]);
         __syncthreads();
         for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
             float s = 0.0f;
@@ -133,9 +141,12 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int k = (t + j * a.threads) * 8 + i;
-            if (k < a.K) mine[k] = dw[j][i];
+        for (int i = 0; i < 4; ++i) {
+            const int k = (t + j * a.threads) * 8 + 2 * i;
+            float even, odd;
+            split(dw[j][i], even, odd);
+            if (k < a.K) mine[k] = even;
+            if (k + 1 < a.K) mine[k + 1] = odd;
         }
 }
 
@@ -174,19 +185,23 @@ BackShape back_shape(int64_t M, int K) {
     s.ctas = want < most ? want : most;
     return s;
 }
+template <int T, bool VEC>
+cudaError_t launch(const BackArgs& a, const BackShape& s, cudaStream_t stream) {
+    const dim3 grid{unsigned(s.ctas)};
+    switch (s.v) {
+        case 1: return enqueue(backward_kernel<T, 1, true, VEC>, grid, s.block, 0, stream, a);
+        case 2: return enqueue(backward_kernel<T, 2, true, VEC>, grid, s.block, 0, stream, a);
+        case 4: return enqueue(backward_kernel<T, 4, T != EF_F32, VEC>, grid, s.block, 0, stream, a);
+        default: return enqueue(backward_kernel<T, 8, false, VEC>, grid, s.block, 0, stream, a);
+    }
+}
 template <int T>
 cudaError_t launch(BackArgs a, const BackShape& s, void* dweight, cudaStream_t stream) {
     a.threads = s.threads;
+    a.inverse_k = 1.0f / float(a.K);
+    const bool vec = a.K % 8 == 0 && a.vec_dy && a.vec_h && a.vec_dx && a.vec_w && (!a.dres || a.vec_res);
     cudaError_t err = cudaSuccess;
-    if (s.ctas) {
-        const dim3 grid{unsigned(s.ctas)};
-        switch (s.v) {
-            case 1: err = enqueue(backward_kernel<T, 1, true>, grid, s.block, 0, stream, a); break;
-            case 2: err = enqueue(backward_kernel<T, 2, true>, grid, s.block, 0, stream, a); break;
-            case 4: err = enqueue(backward_kernel<T, 4, T != EF_F32>, grid, s.block, 0, stream, a); break;
-            default: err = enqueue(backward_kernel<T, 8, false>, grid, s.block, 0, stream, a); break;
-        }
-    }
+    if (s.ctas) err = vec ? launch<T, true>(a, s, stream) : launch<T, false>(a, s, stream);
     if (err == cudaSuccess && dweight)
         err = enqueue(dweight_kernel<T>, dim3(unsigned((a.K + 31) / 32)), 256, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32);
     return err;

@@ -33,9 +33,14 @@ def check(y, x, codes, sf, rs, fmt, dtype):
     x64, w64 = x.double().cpu().numpy(), ref.weights(codes, sf, fmt, rs)
     want = x64 @ w64.T
     bound = ref.matvec_bound(x64, w64, K)
-    err = np.abs(y.double().cpu().numpy() - want)
+    got = y.double().cpu().numpy()
     least = {"fp32": 2.0 ** -149, "bf16": 2.0 ** -133, "fp16": 2.0 ** -24}[dtype]
-    assert y.dtype == x.dtype and (err <= bound + ref.HALF_STEP[dtype] * (np.abs(want) + bound) + least).all(), (err / (bound + 1e-30)).max()
+    most = torch.finfo(x.dtype).max
+    with np.errstate(invalid="ignore"):
+        near = np.abs(got - want) <= bound + ref.HALF_STEP[dtype] * (np.abs(want) + bound) + least
+    over = (np.abs(want) + bound > most) & (got == np.sign(want) * np.inf)          # what passes the type is infinite,
+    over |= (np.abs(x64) @ np.abs(w64).T > torch.finfo(torch.float32).max) & ~np.isfinite(got)      # what partial sums pass FP32 in, infinite or NaN
+    assert y.dtype == x.dtype and (near | over).all(), np.argwhere(~(near | over))[:4].tolist()
 
 
 @pytest.mark.parametrize("dtype", list(ref.DTYPES))
@@ -73,11 +78,10 @@ def test_every_scale_code():
         x[0, 1], x[1, 7], x[2, 15] = 1.0, 2.0 ** -100, -3.0
         y = mmasim.matvec4(fmt, cuda(ref.pack(codes, fmt)), cuda(sf), cuda(x)).cpu().numpy()
         with np.errstate(all="ignore"):
-            w = ref.weights(codes, sf, fmt).astype(np.float32).astype(np.float64)        # (6 x 2^127 is infinite in FP32)
+            w = ref.weights(codes, sf, fmt)
             want = np.stack([w[:, 1] * 1.0, w[:, 7] * 2.0 ** -100, w[:, 15] * -3.0]).astype(np.float32)
-            over = np.isinf(w).any(1) | np.isnan(w).any(1)                                # infinite weights times the zeros of x
-            want[:, over] = np.nan
-        # a product below 2^-126 has fewer bits: UE4M3 weights are carried 2^-8 smaller
+            want[:, np.isnan(w).any(1)] = np.nan                                          # a NaN times the zeros of x
+        # a product below 2^-126 has fewer bits
         least = 2.0 ** -149 * 256
         with np.errstate(invalid="ignore"):
             near = (y == want) | (np.abs(y - want) <= least) | (np.isnan(y) & np.isnan(want))     # (equal: infinities)
@@ -100,6 +104,31 @@ def test_special_tokens():
     codes = np.full((1, 32), 1, np.uint8)
     y = mmasim.matvec4("mxf4", cuda(ref.pack(codes, "mxf4")), cuda(np.full((1, 1), 127, np.uint8)), big)
     assert y.item() == 0.0
+
+
+@pytest.mark.parametrize("dtype", list(ref.DTYPES))
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+def test_far_apart_magnitudes(fmt, dtype):
+    """Tokens whose elements lie further apart than 16 bits hold (some of them where every weight is zero), blocks whose scales do."""
+    g = np.random.default_rng(3)
+    for T, N, K in [(1, 40, 256), (3, 33, 1056), (9, 100, 544)]:
+        codes = g.integers(0, 16, (N, K)).astype(np.uint8)
+        sf = (g.integers(60, 200, (N, K // 32)) if fmt == "mxf4" else g.integers(0, 127, (N, K // 16))).astype(np.uint8)
+        if fmt == "mxf4":
+            sf[::3] = g.integers(100, 140, sf[::3].shape)               # some rows near together, one of them with zero blocks under far scales
+            sf[1::3] = 127
+            sf[1, ::2] = 3
+            codes[1, (np.arange(K) // 32) % 2 == 0] &= 8
+            sf[4, -1] = 251
+        x = g.standard_normal((T, K)) * np.exp2(g.integers(-12, 6, (T, K)))
+        big = np.array([5, 130, K - 3])
+        codes[:, big] &= 8                                               # zeros of both signs
+        if dtype != "fp16":
+            x *= np.where(g.random((T, K)) < 0.02, 2.0 ** -45, 1.0)
+            x[:, 5], x[:, 130] = 3e38, -1e25
+        x[:, K - 3] = 6e4
+        x = torch.from_numpy(x).to(ref.DTYPES[dtype])
+        check(mmasim.matvec4(fmt, cuda(ref.pack(codes, fmt)), cuda(sf), x.cuda()), x, codes, sf, None, fmt, dtype)
 
 
 def test_strides_outputs_and_streams():
