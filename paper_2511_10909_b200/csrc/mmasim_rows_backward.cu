@@ -5,6 +5,8 @@
 // One pass: both sums of a row (h^2 and g h) come from the same loads, so nothing of the forward pass has to be kept but h.  Memory is what
 // bounds it (8 bytes an element in BF16 with a residual).  A CTA walks over rows, a thread keeps its columns and with them its share of
 // dweight in registers; the CTAs' shares go to the workspace, and a second kernel adds them column by column, in one order whatever runs first.
+// The rows to come are on their way into shared memory meanwhile (asynchronous copies; a thread reads what it copied, so that no barrier but
+// the sums' is needed).
 #include "mmasim_quant.cuh"
 
 namespace mmasim {
@@ -43,12 +45,39 @@ __device__ __forceinline__ float2 row_sums(float2 v, int threads, float2* slot) 
     return v;
 }
 
+// The CTA's share of dweight.
+template <int V>
+__device__ __forceinline__ void store_shares(const BackArgs& a, const Pair (&dw)[V][4], float* group_share, int per_cta, int t) {
+    float* mine = a.part + int64_t(blockIdx.x) * a.K;
+    if (V == 1 && a.threads <= 32) {        // several rows at a time: the groups' shares first
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split(dw[0][i], group_share[threadIdx.x * 8 + 2 * i], group_share[threadIdx.x * 8 + 2 * i + 1]);
+        __syncthreads();
+        for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+            float s = 0.0f;
+            for (int g = 0; g < per_cta; ++g) s += group_share[g * a.threads * 8 + k];
+            mine[k] = s;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = (t + j * a.threads) * 8 + 2 * i;
+            float even, odd;
+            split(dw[j][i], even, odd);
+            if (k < a.K) mine[k] = even;
+            if (k + 1 < a.K) mine[k + 1] = odd;
+        }
+}
+
 // HOLD: dy and h stay in registers between the sums and the results; else they are read again (rows too long for that).
 template <int T, int V, bool HOLD, bool VEC>
 __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a) {
     using E = typename Elem<T>::type;
     __shared__ float2 slots[2][16];
-    __shared__ float group_share[8 * 128];
+    __shared__ float group_share[V == 1 ? 8 * 128 : 1];
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
@@ -125,51 +154,170 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
             store8<T, VEC>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, K - at, a.vec_dx);
         }
     }
-    if (!a.part) return;
-    float* mine = a.part + int64_t(blockIdx.x) * a.K;
-    if (a.threads <= 32) {                  // (V = 1) several rows at a time: the groups' shares first
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split(dw[0][i], group_share[threadIdx.x * 8 + 2 * i], group_share[threadIdx.x * 8 + 2 * i + 1]);
-        __syncthreads();
-        for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
-            float s = 0.0f;
-            for (int g = 0; g < per_cta; ++g) s += group_share[g * a.threads * 8 + k];
-            mine[k] = s;
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = (t + j * a.threads) * 8 + 2 * i;
-            float even, odd;
-            split(dw[j][i], even, odd);
-            if (k < a.K) mine[k] = even;
-            if (k + 1 < a.K) mine[k + 1] = odd;
-        }
+    if (a.part) store_shares<V>(a, dw, group_share, per_cta, t);
 }
 
-// dweight: 32 columns a CTA, eight warps over the shares (8192 FP32 additions a column at most).
+// Both sums of the row's threads with half the exchanges: after the first, one half of a warp has one sum and the other the other.
+// `slot`: 32 words of shared memory that nothing else uses.
+__device__ __forceinline__ float2 row_sums_wide(float2 v, int threads, float* slot) {
+    const int lane = threadIdx.x & 31;
+    const bool upper = lane >= 16;
+    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? v.x : v.y, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (threads > 32) {
+        if ((lane & 15) == 0) slot[lane + (threadIdx.x >> 5)] = s;
+        __syncthreads();
+        s = (lane & 15) < threads / 32 ? slot[lane] : 0.0f;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    }
+    return make_float2(__shfl_sync(0xFFFFFFFFu, s, 0), __shfl_sync(0xFFFFFFFFu, s, 16));
+}
+
+// The same for whole eights at multiples of 16 bytes: `depth` rows (2 or 3) of h, dy and dresidual in shared memory, the threads' slots of 16
+// bytes side by side (a thread's own side by side, free of conflicts between banks too, made the copies three times as slow).
+template <int T, int V> constexpr int RING_SLOTS = 3 * V * (Elem<T>::WORDS / 4);
+template <int T, int V>
+__global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackArgs a, const int depth) {
+    using E = typename Elem<T>::type;
+    constexpr int PER = Elem<T>::WORDS / 4, EACH = 16 / sizeof(E);      // slots of an eight, elements of a slot
+    extern __shared__ uint4 ring[];
+    __shared__ float slots[2][32];
+    __shared__ float2 few_slots[1];
+    __shared__ float group_share[V == 1 ? 8 * 128 : 1];
+    after_previous();
+    const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
+    const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
+    const int64_t stride = int64_t(gridDim.x) * per_cta;
+    const uint32_t plane = blockDim.x * 16, stage = plane * RING_SLOTS<T, V>, mine = threadIdx.x * 16, end = mine + depth * stage;
+    uint32_t in = mine, out = mine;                     // of the row to be fetched and to be read next
+    int64_t ahead = int64_t(blockIdx.x) * per_cta + group;
+    const E *dy = static_cast<const E*>(a.dy) + ahead * a.ld_dy + t * 8, *h_at = static_cast<const E*>(a.h) + ahead * a.ld_h + t * 8;
+    const E* res_at = a.dres ? static_cast<const E*>(a.dres) + ahead * a.ld_res + t * 8 : nullptr;
+    E* dx = static_cast<E*>(a.dx) + ahead * a.ld_dx + t * 8;
+    auto fetch = [&]() {
+        if (ahead < a.M) {
+            const uint32_t to = uint32_t(__cvta_generic_to_shared(ring)) + in;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if ((t + j * a.threads) * 8 >= a.K) continue;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int at = j * a.threads * 8 + i * EACH, slot = j * PER + i;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + slot * plane), "l"(h_at + at) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V * PER + slot) * plane), "l"(dy + at) : "memory");
+                    if (a.dres) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (2 * V * PER + slot) * plane), "l"(res_at + at) : "memory");
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        in = in + stage == end ? mine : in + stage;
+        ahead += stride;
+        h_at += stride * a.ld_h;
+        dy += stride * a.ld_dy;
+        res_at += stride * a.ld_res;
+    };
+    for (int i = 1; i < depth; ++i) fetch();
+
+    Pair w[V][4], dw[V][4];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int at = (t + j * a.threads) * 8;
+        load_weight8<T, true>(a.w, a.w_f32, at, a.K - at, true, w[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dw[j][i] = 0;
+    }
+    int turn = 0;
+    for (int64_t first = int64_t(blockIdx.x) * per_cta; first < a.M; first += stride, turn ^= 1) {
+        const int K = first + group < a.M ? a.K : 0;
+        fetch();
+        if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else asm volatile("cp.async.wait_group 1;" ::: "memory");
+        auto take = [&](int which, int j) {
+            Raw<T> r;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(ring) + out + ((which * V + j) * PER + i) * plane);
+                r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
+            }
+            return r;
+        };
+        Pair squares = 0, products = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if ((t + j * a.threads) * 8 >= K) continue;
+            Pair hv[4], gv[4];
+            widen<T>(take(0, j), hv);
+            widen<T>(take(1, j), gv);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                squares = fma2(hv[i], hv[i], squares);
+                products = fma2(mul2(gv[i], w[j][i]), hv[i], products);
+            }
+        }
+        float2 sums, odd;
+        split(squares, sums.x, odd.x);
+        split(products, sums.y, odd.y);
+        sums = make_float2(sums.x + odd.x, sums.y + odd.y);
+        sums = a.threads >= 32 ? row_sums_wide(sums, a.threads, slots[turn]) : row_sums(sums, a.threads, few_slots);       // (two sets of slots: one barrier a row)
+        const float r = inverse_root(__fmaf_rn(sums.x, a.inverse_k, a.eps));
+        const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if ((t + j * a.threads) * 8 >= K) continue;
+            Pair hv[4], gv[4], o[4];        // (read again: held, they cost a third of the CTAs of an SM their place)
+            widen<T>(take(0, j), hv);
+            widen<T>(take(1, j), gv);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                dw[j][i] = fma2(gv[i], mul2(hv[i], rr), dw[j][i]);
+                o[i] = fma2(mul2(gv[i], w[j][i]), rr, mul2(hv[i], c));
+            }
+            if (a.dres) {
+                Pair res[4];
+                widen<T>(take(2, j), res);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = add2(o[i], res[i]);
+            }
+            Raw<T> raw;
+            narrow<T>(o, raw);
+            store8<T, true>(dx + j * a.threads * 8, raw, 8, true);
+        }
+        out = out + stage == end ? mine : out + stage;
+        dx += stride * a.ld_dx;
+    }
+    if (a.part) store_shares<V>(a, dw, group_share, per_cta, t);
+}
+
+// dweight: 32 columns a CTA, 32 warps over the shares.
 template <int T>
-__global__ void __launch_bounds__(256) dweight_kernel(const float* part, int shares, int K, void* dw, int f32) {
-    __shared__ float s[8][32];
+__global__ void __launch_bounds__(1024) dweight_kernel(const float* part, int shares, int K, void* dw, int f32) {
+    __shared__ float s[32][32];
     after_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
     float v = 0.0f;
-    if (k < K)
-        for (int g = warp; g < shares; g += 8) v += part[int64_t(g) * K + k];
+    if (k < K) {
+        for (int g = warp; g < shares; g += 32 * 8) {
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = g + 32 * i < shares ? part[int64_t(g + 32 * i) * K + k] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += p[i];
+        }
+    }
     s[warp][lane] = v;
     __syncthreads();
     if (warp || k >= K) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += s[i][lane];
+    for (int i = 1; i < 32; ++i) v += s[i][lane];
     if (f32) static_cast<float*>(dw)[k] = v;
     else if constexpr (T == EF_F32) static_cast<float*>(dw)[k] = v;
     else if constexpr (T == EF_BF16) static_cast<__nv_bfloat16*>(dw)[k] = __float2bfloat16_rn(v);
     else static_cast<__half*>(dw)[k] = __float2half_rn(v);
 }
 
+// Threads per row, eights per thread, CTAs: what the workspace goes by too, so by sizes alone (whether the call takes the ring or not).
 struct BackShape { int threads, v; unsigned block; int64_t ctas; };
 BackShape back_shape(int64_t M, int K) {
     const int eights = (K + 7) / 8;
@@ -177,16 +325,40 @@ BackShape back_shape(int64_t M, int K) {
     s.v = 1;
     if (eights <= 32) s.threads = eights <= 8 ? 8 : (eights <= 16 ? 16 : 32);
     else {
+        while (s.v < 4 && eights > s.v * 256) s.v *= 2;
         while (eights > s.v * MAX_THREADS) s.v *= 2;
         s.threads = ((eights + s.v - 1) / s.v + 31) / 32 * 32;
     }
     s.block = s.threads > 32 ? unsigned(s.threads) : 128u;
-    const int64_t per_cta = s.threads > 32 ? 1 : 128 / s.threads, want = (M + per_cta - 1) / per_cta, most = 148 * (1024 / s.block);
+    // as many as an SM holds with their rings and registers (BF16 with a residual, CTAs an SM 2 / 3 / 4: 4096 x 4096 32.6 / 41.0 / 36.8 us,
+    // 16384 x 8192 174 / 207 / 183; one eight a thread, 16384 x 1024 46.9 / 37.9 / 34.2), but two rows each: their shares are read again
+    const int64_t per_cta = s.threads > 32 ? 1 : 128 / s.threads, want = (M + per_cta - 1) / per_cta, few = (want + 1) / 2 < 148 ? 148 : (want + 1) / 2;
+    int64_t most = 148 * (s.v > 1 ? 2 : 4);
+    if (most > few) most = few;
     s.ctas = want < most ? want : most;
     return s;
 }
+constexpr size_t RING_MOST = 216 * 1024;
+template <int T, int V>
+cudaError_t launch_ring(const BackArgs& a, const BackShape& s, cudaStream_t stream) {
+    const size_t row = size_t(RING_SLOTS<T, V>) * 16 * s.block;
+    const int depth = 3 * row * (s.ctas / 148 > 1 ? size_t(s.ctas / 148) : 1) <= RING_MOST ? 3 : 2;
+    const size_t smem = depth * row;
+    if (smem > 40 * 1024) {                 // (the sums' slots and the groups' shares come on top)
+        const cudaError_t err = cudaFuncSetAttribute(backward_ring_kernel<T, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(RING_MOST));
+        if (err != cudaSuccess) { cudaGetLastError(); return err; }
+    }
+    return enqueue(backward_ring_kernel<T, V>, dim3(unsigned(s.ctas)), s.block, smem, stream, a, depth);
+}
 template <int T, bool VEC>
 cudaError_t launch(const BackArgs& a, const BackShape& s, cudaStream_t stream) {
+    if constexpr (VEC) {
+        if (size_t(2) * 3 * s.v * (Elem<T>::WORDS / 4) * 16 * s.block <= RING_MOST) {
+            if (s.v == 1) return launch_ring<T, 1>(a, s, stream);
+            if (s.v == 2) return launch_ring<T, 2>(a, s, stream);
+            if (s.v == 4) return launch_ring<T, 4>(a, s, stream);
+        }
+    }
     const dim3 grid{unsigned(s.ctas)};
     switch (s.v) {
         case 1: return enqueue(backward_kernel<T, 1, true, VEC>, grid, s.block, 0, stream, a);
@@ -203,7 +375,7 @@ cudaError_t launch(BackArgs a, const BackShape& s, void* dweight, cudaStream_t s
     cudaError_t err = cudaSuccess;
     if (s.ctas) err = vec ? launch<T, true>(a, s, stream) : launch<T, false>(a, s, stream);
     if (err == cudaSuccess && dweight)
-        err = enqueue(dweight_kernel<T>, dim3(unsigned((a.K + 31) / 32)), 256, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32);
+        err = enqueue(dweight_kernel<T>, dim3(unsigned((a.K + 31) / 32)), 1024, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32);
     return err;
 }
 }  // namespace
