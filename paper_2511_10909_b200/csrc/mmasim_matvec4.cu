@@ -30,6 +30,27 @@ constexpr int STAGE = 2304;                 // bytes of a warp's loads of one st
 constexpr int BLOCK_TOKENS = 2;             // up to so many tokens in columns by block
 constexpr size_t SMEM_MOST = 227 * 1024;
 
+template <int T> constexpr int PARTS = T == EF_F32 ? 3 : 1;
+
+// Places in shared memory: x, a step of zeros, the scales of the columns, by token the steps that are not exact in FP16, the warps' shares of
+// a tile, their loads in flight.  (What the host works out here it need not at the start of every CTA.)
+struct Layout {
+    int steps, pitch;                       // pitch: bytes of a column
+    uint32_t zeros, scales, flags, share, ring;
+};
+// A column has HALF_BYTES per 128 elements: four blocks of 32, 16 bytes more behind two of them, and columns 32 bytes off a multiple of 128, so
+// that the eight lanes of a quarter warp (four blocks of two columns) read from different banks.
+constexpr int HALF_BYTES = HALF * 2 + 16;
+__host__ __device__ inline int block_at(int half, int block) { return half * HALF_BYTES + block * 64 + (block >> 1) * 16; }
+inline size_t layout(int K, int columns, int nt, int stages, Layout* l) {
+    l->steps = (K + STEP - 1) / STEP;
+    l->pitch = (l->steps * (STEP / HALF) * HALF_BYTES + 95) / 128 * 128 + 32;
+    const size_t zeros = size_t(columns) * l->pitch, scales = zeros + 2 * HALF_BYTES, flags = scales + size_t(l->steps) * (STEP / HALF) * nt * 8 * 4;
+    const size_t share = (flags + size_t(columns) * l->steps + 15) / 16 * 16, ring = share + size_t(WARPS) * ROWS * nt * 8 * 4;
+    l->zeros = uint32_t(zeros); l->scales = uint32_t(scales); l->flags = uint32_t(flags); l->share = uint32_t(share); l->ring = uint32_t(ring);
+    return ring + size_t(stages) * WARPS * STAGE;
+}
+
 struct MatvecArgs {
     int N, K, tokens;
     const uint8_t *w, *sf;
@@ -38,31 +59,9 @@ struct MatvecArgs {
     void* y;
     int64_t ldw, ldx, ldy;                  // ldw in bytes
     int vec_x, stages, copy_codes;
-};
-
-template <int T> constexpr int PARTS = T == EF_F32 ? 3 : 1;
-
-// Shared memory: x, a step of zeros, then the scales of its columns, the steps that are not exact in FP16, the warps' shares of a tile, their loads in flight.
-struct Layout {
-    int steps, pitch;                       // pitch: bytes of a column
-    size_t zeros, scales, flags, share, ring, end;
-};
-// A column has HALF_BYTES per 128 elements: four blocks of 32, 16 bytes more behind two of them, and columns 32 bytes off a multiple of 128, so
-// that the eight lanes of a quarter warp (four blocks of two columns) read from different banks.
-constexpr int HALF_BYTES = HALF * 2 + 16;
-__host__ __device__ inline int block_at(int half, int block) { return half * HALF_BYTES + block * 64 + (block >> 1) * 16; }
-__host__ __device__ inline Layout layout(int K, int columns, int nt, int stages) {
+    int tiles, chunks;                      // of 16 rows, and of 32 elements of K
     Layout l;
-    l.steps = (K + STEP - 1) / STEP;
-    l.pitch = (l.steps * (STEP / HALF) * HALF_BYTES + 95) / 128 * 128 + 32;
-    l.zeros = size_t(columns) * l.pitch;    // a step of zeros
-    l.scales = l.zeros + 2 * HALF_BYTES;
-    l.flags = l.scales + size_t(l.steps) * (STEP / HALF) * nt * 8 * 4;
-    l.share = (l.flags + l.steps + 15) / 16 * 16;
-    l.ring = l.share + size_t(WARPS) * ROWS * nt * 8 * 4;
-    l.end = l.ring + size_t(stages) * WARPS * STAGE;
-    return l;
-}
+};
 
 // The tiles and steps of a warp, one after the other: rounds in which groups of `split` warps have a tile each.
 struct Walk {
@@ -422,11 +421,11 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm vola
 __device__ __forceinline__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory"); }
 // Eight elements of a token into its columns, scaled with the others of their 128 (16 threads); false if one of them is not exact in FP16.
 template <int T>
-__device__ __forceinline__ bool stage_x(const Raw<T>& raw, bool in, unsigned char* at, int pitch, float* scale) {
+__device__ __forceinline__ bool stage_x(const Raw<T>& raw, unsigned char* at, int pitch, float* scale) {
     constexpr int P = PARTS<T>;
     if constexpr (T == EF_F16) {
-        if (in) *reinterpret_cast<uint4*>(at) = make_uint4(raw.w[0], raw.w[1], raw.w[2], raw.w[3]);
-        if (in && scale) *scale = 1.0f;
+        *reinterpret_cast<uint4*>(at) = make_uint4(raw.w[0], raw.w[1], raw.w[2], raw.w[3]);
+        if (scale) *scale = 1.0f;
         return true;
     } else {
         Pair p[4];
@@ -459,12 +458,10 @@ __device__ __forceinline__ bool stage_x(const Raw<T>& raw, bool in, unsigned cha
                 }
             }
         }
-        if (in) {
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                *reinterpret_cast<uint4*>(at + q * pitch) = make_uint4(half[q][0], half[q][1], half[q][2], half[q][3]);
-                if (scale) scale[q] = __uint_as_float(uint32_t(127 - max(up, -126) - 12 * q) << 23);
-            }
+        for (int q = 0; q < P; ++q) {
+            *reinterpret_cast<uint4*>(at + q * pitch) = make_uint4(half[q][0], half[q][1], half[q][2], half[q][3]);
+            if (scale) scale[q] = __uint_as_float(uint32_t(127 - max(up, -126) - 12 * q) << 23);
         }
         return lost == 0u;
     }
@@ -476,7 +473,7 @@ struct Kernel {
     using E = typename Elem<T>::type;
     static constexpr int P = PARTS<T>, PER_TOKEN = BLOCKS ? 4 : P, CODES = NV ? 2 : 1, ROW_CODES = STEP / 32 * CODES, STEP_BYTES = STEP / 2;
     const MatvecArgs& a;
-    const Layout l;
+    const Layout& l;
     const int lane, warp, g, t, chunks, tiles, ctas;
     uint32_t ring, ring_end, in, out;                   // stages to be filled and to be read next
     Walk ahead;
@@ -484,9 +481,8 @@ struct Kernel {
     int w_next, codes_next;                             // bytes to the warp's following step
 
     __device__ __forceinline__ explicit Kernel(const MatvecArgs& args)
-        : a(args), l(layout(args.K, args.tokens * P, NT, args.stages)), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g(lane >> 2), t(lane & 3),
-          chunks(args.K / 32), tiles((args.N + ROWS - 1) / ROWS), ctas(gridDim.x) {
-        in = out = ring = uint32_t(l.ring) + warp * (a.stages * STAGE);
+        : a(args), l(args.l), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), g(lane >> 2), t(lane & 3), chunks(args.chunks), tiles(args.tiles), ctas(gridDim.x) {
+        in = out = ring = l.ring + warp * (a.stages * STAGE);
         ring_end = ring + a.stages * STAGE;
         enter(0);
     }
@@ -536,57 +532,77 @@ struct Kernel {
         __syncwarp();
     }
 
-    // x into its columns: 16 threads for the 128 elements of a token that share a scale.  Whether all of it is exact in FP16.
-    static constexpr int BATCH = T == EF_F32 ? 2 : 4;
-    struct Eights {
+    // x into its columns: a warp takes a step of a token at a time, 16 of its threads the 128 elements that share a scale.  The next ones are
+    // on their way meanwhile.  Whether all of it is exact in FP16.
+    static constexpr int BATCH = BLOCKS || T == EF_F32 ? 1 : 4;           // (more of few: more code to be fetched than there is to do)
+    struct Steps {
         Raw<T> raw[BATCH];
-        int tok, o;                                     // of the first, the others 512 eights apart
+        int tok, step;                                  // of the first, the others 16 steps apart
+        __device__ __forceinline__ void settle(int steps) { while (step >= steps) { step -= steps; ++tok; } }
     };
-    __device__ __forceinline__ void ask(Eights& e) const {
-        const int token_eights = l.steps * (STEP / 8);
-        while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
-        int tok = e.tok, o = e.o;
+    __device__ __forceinline__ void ask(Steps& s) const {
+        s.settle(l.steps);
+        int tok = s.tok, step = s.step;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            while (o >= token_eights) { o -= token_eights; ++tok; }
-            const bool there = tok < a.tokens && o * 8 < a.K;
-            e.raw[i] = load8<T, false>(static_cast<const E*>(a.x) + (there ? tok * a.ldx + o * 8 : 0), there ? 8 : 0, a.vec_x);
-            o += WARPS * 32;
+            while (step >= l.steps) { step -= l.steps; ++tok; }
+            const int k = step * STEP + lane * 8;
+            const bool there = tok < a.tokens && k < a.K;
+            s.raw[i] = load8<T, false>(static_cast<const E*>(a.x) + (there ? tok * a.ldx + k : 0), there ? 8 : 0, a.vec_x);
+            step += WARPS;
         }
     }
-    __device__ __forceinline__ bool stage(Eights& e) {
-        const int token_eights = l.steps * (STEP / 8);
+    __device__ __forceinline__ bool stage(Steps& s) {
         bool exact = true;
-        while (true) {
+        while (s.tok < a.tokens) {
+            Steps following;
+            following.tok = s.tok;
+            following.step = s.step + BATCH * WARPS;
+            ask(following);
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
-                if (__any_sync(0xFFFFFFFFu, e.tok < a.tokens)) {
-                    const int half = e.o >> 4;
-                    unsigned char* at = smem + e.tok * P * l.pitch + block_at(half, e.o >> 2 & 3) + (e.o & 3) * 16;
-                    float* scale = (e.o & 15) == 0 ? reinterpret_cast<float*>(smem + l.scales) + half * NT * 8 + e.tok * P : nullptr;
-                    if (!stage_x<T>(e.raw[i], e.tok < a.tokens, at, l.pitch, scale) && e.tok < a.tokens) {
-                        exact = false;
-                        smem[l.flags + half / (STEP / HALF)] = 1;
-                    }
+                if (s.tok < a.tokens) {
+                    const int half = s.step * 2 + (lane >> 4);
+                    unsigned char* at = smem + s.tok * P * l.pitch + block_at(half, lane >> 2 & 3) + (lane & 3) * 16;
+                    float* scale = (lane & 15) == 0 ? reinterpret_cast<float*>(smem + l.scales) + half * NT * 8 + s.tok * P : nullptr;
+                    const bool lost = !__all_sync(0xFFFFFFFFu, stage_x<T>(s.raw[i], at, l.pitch, scale));
+                    if (T != EF_F16 && lane == 0) smem[l.flags + s.tok * l.steps + s.step] = lost;
+                    exact = exact && !lost;
+                    s.step += WARPS;
+                    s.settle(l.steps);
                 }
-                e.o += WARPS * 32;
             }
-            while (e.o >= token_eights) { e.o -= token_eights; ++e.tok; }
-            if (!__any_sync(0xFFFFFFFFu, e.tok < a.tokens)) break;
-            ask(e);
+            s = following;
         }
         return exact;
     }
+    // FP16 as it is, copied without a stop on the way.
+    __device__ __forceinline__ void copy_x(Steps& s) const {
+        for (s.settle(l.steps); s.tok < a.tokens; s.step += WARPS, s.settle(l.steps)) {
+            const int half = s.step * 2 + (lane >> 4), k = s.step * STEP + lane * 8;
+            unsigned char* at = smem + s.tok * P * l.pitch + block_at(half, lane >> 2 & 3) + (lane & 3) * 16;
+            if (k < a.K) copy16(uint32_t(__cvta_generic_to_shared(at)), static_cast<const E*>(a.x) + s.tok * a.ldx + k);
+            else *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+            if ((lane & 15) == 0) reinterpret_cast<float*>(smem + l.scales)[half * NT * 8 + s.tok * P] = 1.0f;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ bool inexact(int step) const {           // of any token
+        bool lost = false;
+        for (int tok = 0; tok < a.tokens; ++tok) lost = lost || smem[l.flags + tok * l.steps + step];
+        return lost;
+    }
 
     // The tile's shares of its warps, put together.
-    __device__ __forceinline__ void finish(const Walk& now, float (&acc)[NT][4]) const {
+    __device__ __forceinline__ float row_scale(const Walk& now) const {        // of the row that this thread puts together (the same one for every token)
+        const int first = threadIdx.x - warp / now.split * now.split * 32;
+        return a.row_scale && first < ROWS * a.tokens && now.tile < tiles ? a.row_scale[min(now.tile * ROWS + (first & (ROWS - 1)), a.N - 1)] : 1.0f;
+    }
+    __device__ __forceinline__ void finish(const Walk& now, float scale, float (&acc)[NT][4]) const {
         constexpr int COLUMNS = BLOCKS ? NT * 2 : NT * 8;               // of a share
         float* const share = reinterpret_cast<float*>(smem + l.share);
         const int split = now.split, group = warp / split, bar = WARPS / split + group;         // barriers 1; 2, 3; 4 .. 7; 8 .. 15
         const int first = threadIdx.x - group * split * 32;
-        float scale = 1.0f;
-        if (a.row_scale && first < ROWS * a.tokens && now.tile < tiles) scale = a.row_scale[min(now.tile * ROWS + (first & (ROWS - 1)), a.N - 1)];      // (the row is the same every time)
         float* mine = share + warp * (ROWS * COLUMNS);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -634,6 +650,7 @@ struct Kernel {
         std::conditional_t<BLOCKS, BlockProduct<NV, NT>, Product<NV, NT>> product;
         Walk now;
         now.begin(0, tiles, ctas);
+        float scale = row_scale(now);
         product.begin(l, a.tokens * P, lane, now.step(), now.split);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) product.acc[nt][0] = product.acc[nt][1] = product.acc[nt][2] = product.acc[nt][3] = 0.0f;
@@ -645,7 +662,7 @@ struct Kernel {
                 const uint32_t at = out + lane * 16;
                 const uint4 va[2] = {load16(at), load16(at + 512)}, vb[2] = {load16(at + 1024), load16(at + 1536)};
                 // the codes of the blocks that the lane decodes (half, row), or that its sums are of
-                const bool wide = GENERAL && T != EF_F16 && smem[l.flags + step], by_block = BLOCKS && !wide;
+                const bool wide = GENERAL && T != EF_F16 && inexact(step), by_block = BLOCKS && !wide;
                 uint32_t codes[2][2];
                 const int block = by_block ? (t & 1) * 2 : t;
 #pragma unroll
@@ -682,8 +699,9 @@ struct Kernel {
             now.base += now.split;
             product.next();
             if (now.base < l.steps) continue;
-            finish(now, product.acc);
+            finish(now, scale, product.acc);
             now.begin(now.following(ctas), tiles, ctas);
+            scale = row_scale(now);
             product.begin(l, a.tokens * P, lane, now.step(), now.split);
         }
     }
@@ -695,19 +713,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) matvec4_kernel(const MatvecArgs
     after_previous();
     Kernel<T, NV, NT, BLOCKS> k(a);
     // x is asked for before the weights' stream begins, and staged before more than a step a warp of it is in front.
-    typename Kernel<T, NV, NT, BLOCKS>::Eights eights;
-    eights.tok = 0;
-    eights.o = threadIdx.x;
-    k.ask(eights);
+    typename Kernel<T, NV, NT, BLOCKS>::Steps steps;
+    steps.tok = 0;
+    steps.step = k.warp;
+    const bool as_it_is = T == EF_F16 && a.vec_x;
+    if (as_it_is) k.copy_x(steps);
+    else k.ask(steps);
     const bool plain = a.K % STEP == 0 && a.copy_codes;
     if (plain) k.template fetch<false>();
     else k.template fetch<true>();
-    const Layout& l = k.l;
-    for (int i = threadIdx.x; i < l.steps; i += WARPS * 32) smem[l.flags + i] = 0;
-    for (int i = threadIdx.x; i < 2 * HALF_BYTES / 4; i += WARPS * 32) reinterpret_cast<uint32_t*>(smem + l.zeros)[i] = 0u;
-    for (int i = threadIdx.x; i < l.steps * (STEP / HALF) * NT * 8; i += WARPS * 32) reinterpret_cast<float*>(smem + l.scales)[i] = 0.0f;
-    __syncthreads();
-    const bool wide = __syncthreads_or(!k.stage(eights));
+    if (BLOCKS && threadIdx.x < 2 * HALF_BYTES / 4) reinterpret_cast<uint32_t*>(smem + a.l.zeros)[threadIdx.x] = 0u;
+    bool exact = true;
+    if (as_it_is) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else exact = k.stage(steps);
+    const bool wide = __syncthreads_or(!exact);
     for (int i = 2; i < a.stages; ++i) {
         if (plain) k.template fetch<false>();
         else k.template fetch<true>();
@@ -722,14 +741,13 @@ cudaError_t launch(const MatvecArgs& a, size_t smem, cudaStream_t stream) {
         const cudaError_t err = cudaFuncSetAttribute(matvec4_kernel<T, NV, NT, BLOCKS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(SMEM_MOST));
         if (err != cudaSuccess) { cudaGetLastError(); return err; }
     }
-    const int tiles = (a.N + ROWS - 1) / ROWS;
-    return enqueue(matvec4_kernel<T, NV, NT, BLOCKS>, dim3(unsigned(tiles < 148 ? tiles : 148)), WARPS * 32, smem, stream, a);
+    return enqueue(matvec4_kernel<T, NV, NT, BLOCKS>, dim3(unsigned(a.tiles < 148 ? a.tiles : 148)), WARPS * 32, smem, stream, a);
 }
 template <int T, bool NV>
 cudaError_t launch(MatvecArgs a, int64_t all, int64_t bytes, cudaStream_t stream) {
     // tokens that read the weights together: 16 columns, as many as shared memory holds beside the shortest ring
     int most = 16 / PARTS<T>;
-    while (layout(a.K, most * PARTS<T>, most * PARTS<T> > 8 ? 2 : 1, 2).end > SMEM_MOST) --most;
+    while (layout(a.K, most * PARTS<T>, most * PARTS<T> > 8 ? 2 : 1, 2, &a.l) > SMEM_MOST) --most;
     const char *x = static_cast<const char*>(a.x), *y = static_cast<const char*>(a.y);
     cudaError_t err = cudaSuccess;
     most = int((all + (all + most - 1) / most - 1) / ((all + most - 1) / most));       // evenly
@@ -740,8 +758,8 @@ cudaError_t launch(MatvecArgs a, int64_t all, int64_t bytes, cudaStream_t stream
         const int columns = a.tokens * PARTS<T>;
         const bool blocks = PARTS<T> == 1 && a.tokens <= BLOCK_TOKENS;
         const int nt = blocks ? (a.tokens <= 2 ? 1 : 2) : (columns <= 8 ? 1 : 2);
-        a.stages = layout(a.K, columns, nt, 4).end <= SMEM_MOST ? 4 : 2;
-        const size_t smem = layout(a.K, columns, nt, a.stages).end;
+        a.stages = layout(a.K, columns, nt, 4, &a.l) <= SMEM_MOST ? 4 : 2;
+        const size_t smem = layout(a.K, columns, nt, a.stages, &a.l);
         if constexpr (PARTS<T> == 1) {
             if (blocks) { err = nt == 1 ? launch<T, NV, 1, true>(a, smem, stream) : launch<T, NV, 2, true>(a, smem, stream); continue; }
         }
@@ -765,6 +783,8 @@ int launch_matvec4(bool nv, int fmt, int64_t T, int64_t N, int64_t K, const void
     a.row_scale = row_scale;
     a.x = x; a.y = y;
     a.ldw = ldw / 2; a.ldx = ldx; a.ldy = ldy;
+    a.tiles = (a.N + ROWS - 1) / ROWS;
+    a.chunks = a.K / 32;
     a.copy_codes = K % STEP == 0 && reinterpret_cast<uintptr_t>(sf) % (nv ? 16 : 8) == 0;
     a.vec_x = (reinterpret_cast<uintptr_t>(x) | uintptr_t(ldx * bytes)) % 16 == 0;
     const cudaError_t err = fmt == EF_F32 ? launch<EF_F32>(nv, a, T, bytes, stream) : fmt == EF_BF16 ? launch<EF_BF16>(nv, a, T, bytes, stream) : launch<EF_F16>(nv, a, T, bytes, stream);
