@@ -92,6 +92,37 @@ template <int T, bool VEC> __device__ __forceinline__ void store8(typename Elem<
         for (int i = 0; i < 8; ++i) if (i < n) s[i] = (unsigned short)(i & 1 ? r.w[i / 2] >> 16 : r.w[i / 2]);
     }
 }
+// Eight elements `step` apart (of `n` left in the row): for rows that no 16-byte access fits, where neighbouring threads take neighbouring
+// elements.
+template <int T> __device__ __forceinline__ Raw<T> load_spread(const typename Elem<T>::type* p, int n, int step) {
+    Raw<T> r;
+    if constexpr (T == EF_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.w[i] = i * step < n ? __float_as_uint(p[i * step]) : 0u;
+    } else {
+        const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = (2 * i * step < n ? uint32_t(s[2 * i * step]) : 0u) | (2 * i * step + step < n ? uint32_t(s[2 * i * step + step]) << 16 : 0u);
+    }
+    return r;
+}
+template <int T> __device__ __forceinline__ void store_spread(typename Elem<T>::type* p, const Raw<T>& r, int n, int step) {
+    if constexpr (T == EF_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i * step < n) p[i * step] = __uint_as_float(r.w[i]);
+    } else {
+        unsigned short* s = reinterpret_cast<unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i * step < n) s[i * step] = (unsigned short)(i & 1 ? r.w[i / 2] >> 16 : r.w[i / 2]);
+    }
+}
+template <int T> __device__ __forceinline__ void load_weight_spread(const void* w, bool f32, int at, int n, int step, Pair (&v)[4]) {
+    if (!w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = both(1.0f);
+    } else if (f32) widen<EF_F32>(load_spread<EF_F32>(static_cast<const float*>(w) + at, n, step), v);
+    else widen<T>(load_spread<T>(static_cast<const typename Elem<T>::type*>(w) + at, n, step), v);
+}
 // Eight weights of a norm: of the rows' type or FP32, or ones.
 template <int T, bool VEC> __device__ __forceinline__ void load_weight8(const void* w, bool f32, int at, int n, bool vec, Pair (&v)[4]) {
     if (!w) {

@@ -60,7 +60,10 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, int threads, uint32_t* s
     return v;
 }
 
-// VEC: rows of whole eights, all of which start on 16 bytes (codes: on their eight or four).
+template <int OUT, bool VEC> constexpr bool SPREAD_ROWS = !VEC && OUT != OUT_MXF4 && OUT != OUT_NVF4;
+
+// VEC: rows of whole eights, all of which start on 16 bytes (codes: on their eight or four).  Other rows: an eight's elements lie a row's threads
+// apart, neighbouring threads take neighbouring elements (a warp the 32 of a block); 4-bit codes, whose rows are whole blocks, as with VEC.
 template <int T, int OUT, int V, bool NORM, bool VEC>
 __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
     using namespace quant;
@@ -74,13 +77,17 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
     // NVF4: two eights side by side where a thread has several, one scale for both (BF16 4096 x 4096: 13.4 us without, 10.9 with; FP32 rows
     // read 64 bytes a thread that way, and a norm of 4096 x 4096 took 47 us, not 37)
     constexpr int SIDE = OUT == OUT_NVF4 && V > 1 && T != EF_F32 ? 2 : 1;
-    auto place = [&](int j) { return (t + j / SIDE * a.threads) * (8 * SIDE) + j % SIDE * 8; };
+    constexpr bool SPREAD = SPREAD_ROWS<OUT, VEC>;
+    auto place = [&](int j) { return SPREAD ? t + j * 8 * a.threads : (t + j / SIDE * a.threads) * (8 * SIDE) + j % SIDE * 8; };
     const int K = row < a.M ? a.K : 0;      // (threads of the last CTA without a row take part in the exchanges between lanes)
     const E* x = static_cast<const E*>(a.x) + row * a.ldx;
 
     Raw<T> h[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = load8<T, VEC>(x + place(j), K - place(j), a.vec_x);
+    for (int j = 0; j < V; ++j) {
+        if constexpr (SPREAD) h[j] = load_spread<T>(x + place(j), K - place(j), a.threads);
+        else h[j] = load8<T, VEC>(x + place(j), K - place(j), a.vec_x);
+    }
     Pair y[NORM ? V : 1][4];                // without a norm the elements stay as they were loaded until their codes are made
     if constexpr (NORM) {
         if (a.residual) {
@@ -88,17 +95,25 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
             E* out = static_cast<E*>(a.h_out) + row * a.ldh;
             Raw<T> res[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) res[j] = load8<T, VEC>(r + place(j), K - place(j), a.vec_r);
+            for (int j = 0; j < V; ++j) {
+                if constexpr (SPREAD) res[j] = load_spread<T>(r + place(j), K - place(j), a.threads);
+                else res[j] = load8<T, VEC>(r + place(j), K - place(j), a.vec_r);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {   // the norm is taken of what is stored: the backward pass has nothing else
                 add_to<T>(h[j], res[j]);
-                if (place(j) < K) store8<T, VEC>(out + place(j), h[j], K - place(j), a.vec_h);
+                if constexpr (SPREAD) store_spread<T>(out + place(j), h[j], K - place(j), a.threads);
+                else if (place(j) < K) store8<T, VEC>(out + place(j), h[j], K - place(j), a.vec_h);
             }
         }
         constexpr bool EARLY = V <= 2;      // asked for before the row's threads wait for one another, where the registers hold them
         Pair w[EARLY ? V : 1][4];
+        auto weight = [&](int j, Pair (&to)[4]) {
+            if constexpr (SPREAD) load_weight_spread<T>(a.w, a.w_f32, place(j), K - place(j), a.threads, to);
+            else load_weight8<T, VEC>(a.w, a.w_f32, place(j), K - place(j), a.vec_w, to);
+        };
 #pragma unroll
-        for (int j = 0; j < V && EARLY; ++j) load_weight8<T, VEC>(a.w, a.w_f32, place(j), K - place(j), a.vec_w, w[j]);
+        for (int j = 0; j < V && EARLY; ++j) weight(j, w[j]);
         Pair squares = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -112,7 +127,7 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
         // (behind the row's end: zeros times zeros, and where r is not finite no element of the row is a number)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if constexpr (!EARLY) load_weight8<T, VEC>(a.w, a.w_f32, place(j), K - place(j), a.vec_w, w[0]);
+            if constexpr (!EARLY) weight(j, w[0]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[j][i] = mul2(mul2(y[j][i], r), w[EARLY ? j : 0][i]);
         }
@@ -124,7 +139,8 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
             const int at = place(j);
             Raw<T> o;
             narrow<T>(y[j], o);
-            if (at < K) store8<T, VEC>(static_cast<E*>(a.out) + row * a.ldo + at, o, K - at, a.vec_o);
+            if constexpr (SPREAD) store_spread<T>(static_cast<E*>(a.out) + row * a.ldo + at, o, K - at, a.threads);
+            else if (at < K) store8<T, VEC>(static_cast<E*>(a.out) + row * a.ldo + at, o, K - at, a.vec_o);
         }
         return;
     }
@@ -159,7 +175,17 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
         }
         bool zero = false;                  // FP4 has no code for a block without numbers
         if constexpr (OUT == OUT_FP8) by.apply(v[0]);
-        if constexpr (OUT == OUT_MX8 || OUT == OUT_MXF4) {
+        if constexpr (SPREAD && OUT == OUT_MX8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float lo, hi;
+                split(v[0][i / 2], lo, hi);
+                const int e = at + i * a.threads;
+                const uint32_t code = e8m0_code(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(i & 1 ? hi : lo) & 0x7FFFFFFFu), a.e5m2 ? 15 : 8);
+                v[0][i / 2] = i & 1 ? pair(lo, __fmul_rn(hi, e8m0_inverse(code))) : pair(__fmul_rn(lo, e8m0_inverse(code)), hi);
+                if ((t & 31) == 0 && e < K) a.sf[row * a.ld_sf + e / 32] = uint8_t(code);
+            }
+        } else if constexpr (OUT == OUT_MX8 || OUT == OUT_MXF4) {
             uint32_t top = largest(0u, v[0]);
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
@@ -185,10 +211,10 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
         if constexpr (OUT == OUT_FP8 || OUT == OUT_MX8) {
             const uint2 c = a.e5m2 ? codes_e5m2(v[0]) : codes_e4m3(v[0]);
             uint8_t* p = static_cast<uint8_t*>(a.out) + row * a.ldo + at;
-            if (VEC || (a.vec_o && at + 8 <= K)) *reinterpret_cast<uint2*>(p) = c;
+            if constexpr (VEC) *reinterpret_cast<uint2*>(p) = c;
             else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (at + i < K) p[i] = uint8_t((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+                for (int i = 0; i < 8; ++i) if (at + i * a.threads < K) p[i * a.threads] = uint8_t((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
             }
         } else {
             uint8_t* p = static_cast<uint8_t*>(a.out) + (row * a.ldo + at) / 2;
@@ -211,10 +237,10 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
 // 22.2, E4M3 rows 13.7 / 11.0 / 9.9; norm of 16384 x 8192 into E4M3 with 512 / 256 threads 170 / 138.
 constexpr int64_t FEW_ROWS = 296;
 struct Shape { int threads, v; };
-inline Shape shape(int64_t M, int K, bool norm) {
+inline Shape shape(int64_t M, int K, bool norm, bool whole_warps) {
     const int eights = (K + 7) / 8;
-    if (eights <= 8) return {8, 1};
-    if (eights <= 16) return {16, 1};
+    if (eights <= 8 && !whole_warps) return {8, 1};
+    if (eights <= 16 && !whole_warps) return {16, 1};
     if (eights <= 32) return {32, 1};
     int v = 1;
     while (M > FEW_ROWS && v < 4 && eights > v * (norm ? 256 : 128)) v *= 2;
@@ -235,23 +261,23 @@ cudaError_t launch_out(const Args& a, int v, cudaStream_t stream) {
     }
 }
 template <int T, int OUT>
-cudaError_t launch_out(const Args& a, int v, bool norm, cudaStream_t stream) {
+cudaError_t launch_out(Args a, bool norm, cudaStream_t stream) {
     const bool vec = a.K % 8 == 0 && a.vec_x && a.vec_o && a.vec_w && (!a.residual || (a.vec_r && a.vec_h));
-    if constexpr (OUT != OUT_PLAIN)
-        if (!norm) return vec ? launch_out<T, OUT, false, true>(a, v, stream) : launch_out<T, OUT, false, false>(a, v, stream);
-    return vec ? launch_out<T, OUT, true, true>(a, v, stream) : launch_out<T, OUT, true, false>(a, v, stream);
-}
-template <int T>
-cudaError_t launch_type(Args a, int out, bool norm, cudaStream_t stream) {
-    const Shape s = shape(a.M, a.K, norm);
+    const Shape s = shape(a.M, a.K, norm, !vec && SPREAD_ROWS<OUT, false>);
     a.threads = s.threads;
     a.inverse_k = 1.0f / float(a.K);
+    if constexpr (OUT != OUT_PLAIN)
+        if (!norm) return vec ? launch_out<T, OUT, false, true>(a, s.v, stream) : launch_out<T, OUT, false, false>(a, s.v, stream);
+    return vec ? launch_out<T, OUT, true, true>(a, s.v, stream) : launch_out<T, OUT, true, false>(a, s.v, stream);
+}
+template <int T>
+cudaError_t launch_type(const Args& a, int out, bool norm, cudaStream_t stream) {
     switch (out) {
-        case OUT_PLAIN: return launch_out<T, OUT_PLAIN>(a, s.v, norm, stream);
-        case OUT_FP8: return launch_out<T, OUT_FP8>(a, s.v, norm, stream);
-        case OUT_MX8: return launch_out<T, OUT_MX8>(a, s.v, norm, stream);
-        case OUT_MXF4: return launch_out<T, OUT_MXF4>(a, s.v, norm, stream);
-        default: return launch_out<T, OUT_NVF4>(a, s.v, norm, stream);
+        case OUT_PLAIN: return launch_out<T, OUT_PLAIN>(a, norm, stream);
+        case OUT_FP8: return launch_out<T, OUT_FP8>(a, norm, stream);
+        case OUT_MX8: return launch_out<T, OUT_MX8>(a, norm, stream);
+        case OUT_MXF4: return launch_out<T, OUT_MXF4>(a, norm, stream);
+        default: return launch_out<T, OUT_NVF4>(a, norm, stream);
     }
 }
 

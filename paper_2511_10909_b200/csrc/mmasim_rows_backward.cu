@@ -46,30 +46,33 @@ __device__ __forceinline__ float2 row_sums(float2 v, int threads, float2* slot) 
 }
 
 // The CTA's share of dweight.
-template <int V>
+template <int V, bool VEC>
 __device__ __forceinline__ void store_shares(const BackArgs& a, const Pair (&dw)[V][4], float* group_share, int per_cta, int t) {
     float* mine = a.part + int64_t(blockIdx.x) * a.K;
-    if (V == 1 && a.threads <= 32) {        // several rows at a time: the groups' shares first
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split(dw[0][i], group_share[threadIdx.x * 8 + 2 * i], group_share[threadIdx.x * 8 + 2 * i + 1]);
-        __syncthreads();
-        for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
-            float s = 0.0f;
-            for (int g = 0; g < per_cta; ++g) s += group_share[g * a.threads * 8 + k];
-            mine[k] = s;
-        }
-        return;
-    }
+    const bool groups = V == 1 && a.threads <= 32;      // several rows at a time: the groups' shares first
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int k = (t + j * a.threads) * 8 + 2 * i;
+            const int k = VEC ? (t + j * a.threads) * 8 + 2 * i : t + (j * 8 + 2 * i) * a.threads, next = VEC ? 1 : a.threads;
             float even, odd;
             split(dw[j][i], even, odd);
-            if (k < a.K) mine[k] = even;
-            if (k + 1 < a.K) mine[k + 1] = odd;
+            if (groups) {
+                float* to = group_share + threadIdx.x / a.threads * a.threads * 8;
+                to[k] = even;
+                to[k + next] = odd;
+            } else {
+                if (k < a.K) mine[k] = even;
+                if (k + next < a.K) mine[k + next] = odd;
+            }
         }
+    if (!groups) return;
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+        float s = 0.0f;
+        for (int g = 0; g < per_cta; ++g) s += group_share[g * a.threads * 8 + k];
+        mine[k] = s;
+    }
 }
 
 // HOLD: dy and h stay in registers between the sums and the results; else they are read again (rows too long for that).
@@ -81,6 +84,16 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
+    // (VEC: an eight side by side; else its elements a row's threads apart, neighbouring threads at neighbouring elements)
+    auto place = [&](int j) { return VEC ? (t + j * a.threads) * 8 : t + j * 8 * a.threads; };
+    auto load = [&](const E* p, int at, int K) {
+        if constexpr (VEC) return load8<T, true>(p + at, K - at, true);
+        else return load_spread<T>(p + at, K - at, a.threads);
+    };
+    auto weight = [&](int at, int K, Pair (&to)[4]) {
+        if constexpr (VEC) load_weight8<T, true>(a.w, a.w_f32, at, K - at, true, to);
+        else load_weight_spread<T>(a.w, a.w_f32, at, K - at, a.threads, to);
+    };
     Pair dw[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -95,24 +108,24 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
         if constexpr (HOLD) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int at = (t + j * a.threads) * 8;
-                h_raw[j] = load8<T, VEC>(h + at, K - at, a.vec_h);
-                dy_raw[j] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
-                if (a.dres) res_raw[j] = load8<T, VEC>(static_cast<const E*>(a.dres) + row * a.ld_res + at, K - at, a.vec_res);
+                const int at = place(j);
+                h_raw[j] = load(h, at, K);
+                dy_raw[j] = load(dy, at, K);
+                if (a.dres) res_raw[j] = load(static_cast<const E*>(a.dres) + row * a.ld_res, at, K);
             }
         }
         Pair squares = 0, products = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int at = (t + j * a.threads) * 8;
+            const int at = place(j);
             if constexpr (!HOLD) {
-                h_raw[0] = load8<T, VEC>(h + at, K - at, a.vec_h);
-                dy_raw[0] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
+                h_raw[0] = load(h, at, K);
+                dy_raw[0] = load(dy, at, K);
             }
             Pair hv[4], g[4], w[4];
             widen<T>(h_raw[HOLD ? j : 0], hv);
             widen<T>(dy_raw[HOLD ? j : 0], g);
-            load_weight8<T, VEC>(a.w, a.w_f32, at, K - at, a.vec_w, w);
+            weight(at, K, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 squares = fma2(hv[i], hv[i], squares);
@@ -127,17 +140,17 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
         const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int at = (t + j * a.threads) * 8;
+            const int at = place(j);
             if (at >= K) continue;
             if constexpr (!HOLD) {
-                h_raw[0] = load8<T, VEC>(h + at, K - at, a.vec_h);
-                dy_raw[0] = load8<T, VEC>(dy + at, K - at, a.vec_dy);
-                if (a.dres) res_raw[0] = load8<T, VEC>(static_cast<const E*>(a.dres) + row * a.ld_res + at, K - at, a.vec_res);
+                h_raw[0] = load(h, at, K);
+                dy_raw[0] = load(dy, at, K);
+                if (a.dres) res_raw[0] = load(static_cast<const E*>(a.dres) + row * a.ld_res, at, K);
             }
             Pair hv[4], g[4], w[4], out[4];
             widen<T>(h_raw[HOLD ? j : 0], hv);
             widen<T>(dy_raw[HOLD ? j : 0], g);
-            load_weight8<T, VEC>(a.w, a.w_f32, at, K - at, a.vec_w, w);
+            weight(at, K, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 dw[j][i] = fma2(g[i], mul2(hv[i], rr), dw[j][i]);
@@ -151,10 +164,11 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
             }
             Raw<T> o;
             narrow<T>(out, o);
-            store8<T, VEC>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, K - at, a.vec_dx);
+            if constexpr (VEC) store8<T, true>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, 8, true);
+            else store_spread<T>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, K - at, a.threads);
         }
     }
-    if (a.part) store_shares<V>(a, dw, group_share, per_cta, t);
+    if (a.part) store_shares<V, VEC>(a, dw, group_share, per_cta, t);
 }
 
 // Both sums of the row's threads with half the exchanges: after the first, one half of a warp has one sum and the other the other.
@@ -287,7 +301,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         out = out + stage == end ? mine : out + stage;
         dx += stride * a.ld_dx;
     }
-    if (a.part) store_shares<V>(a, dw, group_share, per_cta, t);
+    if (a.part) store_shares<V, true>(a, dw, group_share, per_cta, t);
 }
 
 // dweight: 32 columns a CTA, 32 warps over the shares.

@@ -149,20 +149,24 @@ def test_rms_norm_of_special_rows():
     assert torch.isnan(y).all()             # 0 / 0
 
 
+def check_backward(dx, dw, dy, x, w, res, dtype, eps):
+    dx64, dw64, dx_bound, dw_bound = ref.rms_norm_backward(np64(dy), np64(x), None if w is None else np64(w), None if res is None else np64(res), eps)
+    half, least = ref.HALF_STEP[dtype], {"fp32": 2.0 ** -149, "bf16": 2.0 ** -133, "fp16": 2.0 ** -24}[dtype]
+    err = np.abs(np64(dx) - dx64)
+    assert (err <= dx_bound + half * (np.abs(dx64) + dx_bound) + least).all(), (x.shape, err.max())
+    wh = half if w is None or w.dtype != torch.float32 else ref.HALF_STEP["fp32"]
+    assert dw.dtype == (x.dtype if w is None else w.dtype)
+    err = np.abs(np64(dw) - dw64)
+    assert (err <= dw_bound + wh * (np.abs(dw64) + dw_bound) + least).all(), (x.shape, err.max())
+
+
 @pytest.mark.parametrize("dtype", list(ref.DTYPES))
 def test_rms_norm_backward(dtype):
     for i, (M, K) in enumerate(SIZES + [(700, 64), (2000, 40), (300, 520), (650, 1111), (400, 2048)]):
         x, res, w, _ = norm_case(M, K, dtype, i % 2 == 0, [None, False, True][i % 3], seed=7)
         dy = rows(M, K, dtype, 9, 0.1)
         dx, dw = mmasim.rms_norm_backward(dy.cuda(), x.cuda(), None if w is None else w.cuda(), None if res is None else res.cuda(), eps=1e-5)
-        dx64, dw64, dx_bound, dw_bound = ref.rms_norm_backward(np64(dy), np64(x), None if w is None else np64(w), None if res is None else np64(res), float(np.float32(1e-5)))
-        half, least = ref.HALF_STEP[dtype], {"fp32": 2.0 ** -149, "bf16": 2.0 ** -133, "fp16": 2.0 ** -24}[dtype]
-        err = np.abs(np64(dx) - dx64)
-        assert (err <= dx_bound + half * (np.abs(dx64) + dx_bound) + least).all(), (M, K, err.max())
-        wh = half if w is None or w.dtype != torch.float32 else ref.HALF_STEP["fp32"]
-        assert dw.dtype == (x.dtype if w is None else w.dtype)
-        err = np.abs(np64(dw) - dw64)
-        assert (err <= dw_bound + wh * (np.abs(dw64) + dw_bound) + least).all(), (M, K, err.max())
+        check_backward(dx, dw, dy, x, w, res, dtype, float(np.float32(1e-5)))
 
 
 def test_backward_is_the_gradient_of_the_forward_pass():
@@ -216,18 +220,16 @@ def test_strides_and_alignment(fmt, lead, off):
             out = mmasim.Quantized(around[:, :K // per_byte], y0.sf.clone() if y0.sf is not None else None, y0.row_scale.clone() if y0.row_scale is not None else None)
         y1, h1b = mmasim.rms_norm(strided(x, lead, off), strided(w.view(1, -1), 0, off)[0], strided(res, lead, off), fmt=fmt, residual_out=h1, out=out)
         assert h1b is h1 and torch.equal(h1, h0)
+        check_norm(y1, h1, x, res, w, h, dtype, fmt, float(np.float32(1e-6)))           # (the squares' sum has another order)
         if fmt is None:
-            assert y1 is out and torch.equal(y1, y0)
+            assert y1 is out
         else:
-            assert torch.equal(y1.codes, y0.codes) and (around[:, K // per_byte:] == 0xA5).all()
-            for a, b in zip(y0[1:], y1[1:]):
-                assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+            assert (around[:, K // per_byte:] == 0xA5).all()
             q0, q1 = mmasim.quantize(x.cuda(), fmt), mmasim.quantize(strided(x, lead, off), fmt)
             assert all(a is b or torch.equal(a, b) for a, b in zip(q0, q1))
         dy = rows(M, K, dtype, 3)
-        d0, w0 = mmasim.rms_norm_backward(dy.cuda(), h0, w.cuda(), res.cuda())
         d1, w1 = mmasim.rms_norm_backward(strided(dy, lead, off), h1, strided(w.view(1, -1), 0, off)[0], strided(res, lead, off), dx=strided(torch.zeros_like(x), lead, off))
-        assert torch.equal(d0, d1) and torch.equal(w0, w1)
+        check_backward(d1, w1, dy, h, w, res, dtype, float(np.float32(1e-6)))
 
 
 def test_rows_far_apart():
