@@ -2,21 +2,27 @@
 //
 //   y[t, n] = row_scale[n] * sum over k of x[t, k] * e2m1(W[n, k]) * sf[n, k / kb]          in FP32
 //
-// What bounds it is reading the weights once: 46 of them per clock and SM at the memory's rate.  The products go to the warp-level matrix
-// instruction (exact products, FP32 sums), 16 rows of weights against columns of x, so that a weight costs its decoding and little else:
-// in FP16 one conversion for two codes and one multiplication for two scales, both exact (E2M1 times UE4M3 has six bits; the E8M0 scales of
-// four neighbouring blocks enter relative to their largest, which is applied to the sum).  64 weights of a lane take about 105 instructions;
-// with the codes shifted into place for BF16 they took 190, and that bound the kernel (28672 x 8192, one token: 52 us).
+// What should bound it is reading the weights once: 46 of them per clock and SM at the memory's rate.  The products go to the warp-level matrix
+// instruction (exact products, FP32 sums), 16 rows of weights against columns of x, so that a weight costs its decoding and little else: one
+// conversion into FP16 for two codes.  The scales multiply
+//   - sums, where the tokens are few (one or two of 16 bits): a token has four of the instruction's eight columns, one for each of the four
+//     blocks of 32 that a warp's lanes have of 128 elements, so that sums come by block (BlockProduct);
+//   - weights, else: one multiplication for two, exact in FP16 (E2M1 times UE4M3 has six bits; the E8M0 scales of four neighbouring blocks enter
+//     relative to their largest, which multiplies the sum) (Product).
+// 256 elements of 16 rows take a warp 274 instructions the first way (NVFP4, one token) and 337 the second.  Codes shifted into place by
+// integer instructions for BF16, scaled there, took 380 (28672 x 8192, one token: 52 us, now 30).
 //
-// x is staged once per CTA in shared memory, a column of FP16 numbers per token (FP32: three), scaled by a power of two per 128 elements so
-// that the largest is in 2^14 .. 2^15.  Elements of BF16 down to 2^-32 of the largest of their 128 are exact that way, of FP32 to 2^-39.
-// 128 elements of which one is not exact go through BF16 and its wider exponents instead, from x itself (FP32: three parts), with the
-// codes moved to the lowest bits of a BF16 word's exponent - a number 2^-126 times its value.
+// x is staged once per CTA in shared memory, a column of FP16 numbers per token (FP32: three, each with what the one before left), scaled by a
+// power of two per 128 elements so that the largest is in 2^14 .. 2^15.  Elements of BF16 down to 2^-32 of the largest of their 128 are exact
+// that way, of FP32 to 2^-39.  256 elements of which one is not exact go through BF16 and its wider exponents instead, from x itself (FP32:
+// three parts), with the codes moved to the lowest bits of a BF16 word's exponent - a number 2^-126 times its value.
 // The instruction's sums truncate below 2^-24 of their largest term, so they are taken over 128 elements and added up in FP32.
 //
-// One CTA an SM walks over tiles of 16 rows; its warps split K (128 elements in turn) among the 32, 16, 8 or 4 of them that share a tile, by
-// how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next step in flight, over
-// the ends of tiles too.
+// One CTA an SM walks over tiles of 16 rows; its warps split K (256 elements in turn) among the 16, 8, 4 or 2 of them that share a tile, by
+// how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next three steps in flight
+// into its own part of shared memory, over the ends of tiles too (asynchronous copies; loads into registers came 3.5 us late).
+// Where it ends: 28672 x 8192 NVFP4, one token, 30.3 us, 0.67 of the copy rate (the copies alone 25.9: 2.5 us until x is staged and the first
+// tile begun, 7 % for tiles that do not fill the last round; then 2.6 instructions per clock and scheduler quarter).
 #include <type_traits>
 #include "mmasim_quant.cuh"
 

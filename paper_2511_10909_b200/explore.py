@@ -1,6 +1,6 @@
 """Workaround and design-space exploration (Sections 6.3 and 7) on top of the library's entry points.
 
-Three experiments, all at GEMM scale on the GPU, each returning the deviation statistics of `accuracy.deviation_stats`
+Four experiments, all at GEMM scale on the GPU, each returning the deviation statistics of `accuracy.deviation_stats`
 against the FP64 real result:
 
 * `design_sweep`    - hypothetical T-FDPA units: the registry row of a model with other (L_max, F, rho), made by
@@ -8,6 +8,9 @@ against the FP64 real result:
 * `chunk_sweep`     - the FP32-promotion workaround for low-precision accumulation with chunk sizes other than 128;
 * `fp8_via_fp16`    - the workaround that feeds FP8 data to the FP16 instruction (every E4M3 / E5M2 value is an FP16
                       value): the same architecture's FP16 row evaluated on the widened words.
+
+* `quantised_layer`   - a network's layer (norm, quantisation, product) under a unit's arithmetic: what its formats cost, what
+                      the unit costs on top, and what 4-bit weights cost alone.
 
 * `b200_fp8_mma_sync` - what the B200's own warp-level FP8 instruction computes (found with the probes of clfp.py and
                       confirmed bit for bit against `mmasim_hw_mma`): that workaround, in hardware.
@@ -82,6 +85,56 @@ def fp8_via_fp16(arch: str, fmt: str, A, B, C=None, acc: str = "fp32", ref=None)
     s16 = accuracy.deviation_stats(via, widen_fp8_to_fp16(fmt, A), widen_fp8_to_fp16(fmt, B), C, ref)
     s16.update(model=repr(via))
     return {"native": s8, "via_fp16": s16}
+
+
+def dequantised(q: mmasim.Quantized, fmt: str):
+    """The values that a quantised matrix stands for: an FP64 CUDA tensor."""
+    import torch
+    if fmt in ("mxf4", "nvf4"):
+        v = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=q.codes.device)
+        v = torch.cat([v, -v])[torch.stack([q.codes & 15, q.codes >> 4], 2).view(q.codes.shape[0], -1).int()]
+    else:
+        v = accuracy.widen(fmt[-4:], q.codes)
+    if q.sf is not None:
+        sf = q.sf.view(torch.float8_e4m3fn).double() if fmt == "nvf4" else torch.ldexp(torch.ones_like(q.sf, dtype=torch.float64), q.sf.int() - 127)
+        v = v * sf.repeat_interleave(mmasim.SCALE_BLOCK[fmt], dim=1)[:, :v.shape[1]]
+    return v if q.row_scale is None else v * q.row_scale.double()[:, None]
+
+
+def quantised_layer(x, gain, W, rows=(("hopper", "e4m3"), ("blackwell", "e4m3"), ("blackwell", "mxe4m3"), ("blackwell", "mxf4"), ("blackwell", "nvf4")),
+                    residual=None, eps: float = 1e-6) -> dict:
+    """y = rms_norm(x + residual, gain) W^T of a network's layer, for every (architecture, format) of ``rows``: activations by
+    `mmasim.rms_norm`, weights by `mmasim.quantize` into the format, their product under the unit's model with an FP32
+    accumulator.  Statistics (as `accuracy.deviation_stats`) of three deviations:
+      format       the exact product of the quantised operands from that of the unquantised ones, both in FP64;
+      unit         the unit's product from the exact product of the same operands;
+      weight_only  (4-bit formats) `mmasim.matvec4` of the quantised weights and the unquantised activations from the
+                   unquantised product.
+    x, residual: tokens x K, W: N x K, of one type (FP32, BF16, FP16); gain: K."""
+    import torch
+    fp64 = mmasim.Model("ampere", "fp64", "fp64")
+    product = lambda a, b: mmasim.gemm(fp64, a.contiguous().view(torch.int64), b.contiguous().view(torch.int64)).view(torch.float64)
+    y, h = mmasim.rms_norm(x, gain, residual, eps=eps)
+    h64 = (x if h is None else h).double()
+    y64 = h64 / (h64.square().mean(1, keepdim=True) + eps).sqrt() * gain.double()
+    real = product(y64, W.double())
+    words = lambda t: t.float().contiguous().view(torch.int32)
+    out = {}
+    for arch, fmt in rows:
+        q, w = mmasim.rms_norm(x, gain, residual, eps=eps, fmt=fmt)[0], mmasim.quantize(W, fmt)
+        kw = {}
+        if q.sf is not None:
+            kw.update(sfa=q.sf, sfb=w.sf)
+        if q.row_scale is not None:
+            kw.update(row_scale=q.row_scale, col_scale=w.row_scale)
+        D = mmasim.gemm(mmasim.Model(arch, fmt, "fp32"), q.codes, w.codes, K=x.shape[1], **kw)
+        kernel = mmasim.last_kernel()
+        exact = product(dequantised(q, fmt), dequantised(w, fmt))
+        s = {"format": _stats("fp32", words(exact), real), "unit": _stats("fp32", D, exact), "kernel": kernel}
+        if fmt in ("mxf4", "nvf4"):
+            s["weight_only"] = _stats("fp32", words(mmasim.matvec4(fmt, w.codes, w.sf, y, w.row_scale)), real)
+        out[arch, fmt] = s
+    return out
 
 
 def b200_fp8_mma_sync(fmt: str, A, B, C=None, b_fmt: str | None = None):
