@@ -164,7 +164,7 @@ int launch_deviation_end(int acc, int64_t M, int64_t N, int64_t K, const void* C
 int launch_reference_fp64(int fmt, int acc, int64_t M, int64_t N, int64_t K, const void* A, const void* B, const void* C, double* ref, cudaStream_t stream);
 // mmasim_rows.cuh, mmasim_rows_backward.cu, mmasim_matvec4.cu (arguments checked; leading dimensions of args 0 = packed)
 constexpr int64_t ROWS_MAX_K = 32768;           // what a CTA's registers hold of a row
-constexpr int64_t MATVEC_MAX_K_F32 = 28672;     // what shared memory holds of an FP32 token in three parts
+constexpr int64_t MATVEC_MAX_K_F32 = 20480;     // what shared memory holds of an FP32 token in three parts
 int launch_rows(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_args& p, bool norm, cudaStream_t stream);
 size_t rms_norm_backward_workspace(int64_t M, int64_t K);
 int launch_rms_norm_backward(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_backward_args& p, cudaStream_t stream);

@@ -9,8 +9,7 @@
 //     blocks of 32 that a warp's lanes have of 128 elements, so that sums come by block (BlockProduct);
 //   - weights, else: one multiplication for two, exact in FP16 (E2M1 times UE4M3 has six bits; the E8M0 scales of four neighbouring blocks enter
 //     relative to their largest, which multiplies the sum) (Product).
-// 256 elements of 16 rows take a warp 274 instructions the first way (NVFP4, one token) and 337 the second.  Codes shifted into place by
-// integer instructions for BF16, scaled there, took 380 (28672 x 8192, one token: 52 us, now 30).
+// 256 elements of 16 rows take a warp 274 instructions the first way (NVFP4, one token) and 337 the second.
 //
 // x is staged once per CTA in shared memory, a column of FP16 numbers per token (FP32: three, each with what the one before left), scaled by a
 // power of two per 128 elements so that the largest is in 2^14 .. 2^15.  Elements of BF16 down to 2^-32 of the largest of their 128 are exact
@@ -20,7 +19,8 @@
 //
 // One CTA an SM walks over tiles of 16 rows; its warps split K (256 elements in turn) among the 16, 8, 4 or 2 of them that share a tile, by
 // how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next three steps in flight
-// into its own part of shared memory, over the ends of tiles too (asynchronous copies; loads into registers came 3.5 us late).
+// into its own part of shared memory, over the ends of tiles too (28672 x 8192: 49 us with these asynchronous copies where loads into registers,
+// as far ahead, took 66).
 // Where it ends: 28672 x 8192 NVFP4, one token, 30.3 us, 0.67 of the copy rate (the copies alone 25.9: 2.5 us until x is staged and the first
 // tile begun, 7 % for tiles that do not fill the last round; then 2.6 instructions per clock and scheduler quarter).
 #include <type_traits>
@@ -47,8 +47,8 @@ struct Layout {
 // A column has HALF_BYTES per 128 elements: four blocks of 32, 16 bytes more behind two of them, and columns 32 bytes off a multiple of 128, so
 // that the eight lanes of a quarter warp (four blocks of two columns) read from different banks.
 constexpr int HALF_BYTES = HALF * 2 + 16;
-__host__ __device__ inline int block_at(int half, int block) { return half * HALF_BYTES + block * 64 + (block >> 1) * 16; }
-inline size_t layout(int K, int columns, int nt, int stages, Layout* l) {
+__host__ __device__ constexpr int block_at(int half, int block) { return half * HALF_BYTES + block * 64 + (block >> 1) * 16; }
+constexpr size_t layout(int K, int columns, int nt, int stages, Layout* l) {
     l->steps = (K + STEP - 1) / STEP;
     l->pitch = (l->steps * (STEP / HALF) * HALF_BYTES + 95) / 128 * 128 + 32;
     const size_t zeros = size_t(columns) * l->pitch, scales = zeros + 2 * HALF_BYTES, flags = scales + size_t(l->steps) * (STEP / HALF) * nt * 8 * 4;
@@ -56,6 +56,11 @@ inline size_t layout(int K, int columns, int nt, int stages, Layout* l) {
     l->zeros = uint32_t(zeros); l->scales = uint32_t(scales); l->flags = uint32_t(flags); l->share = uint32_t(share); l->ring = uint32_t(ring);
     return ring + size_t(stages) * WARPS * STAGE;
 }
+constexpr size_t least_layout(int64_t K, int columns) {
+    Layout l = {};
+    return layout(int(K), columns, 1, 2, &l);
+}
+static_assert(least_layout(ROWS_MAX_K, PARTS<EF_BF16>) <= SMEM_MOST && least_layout(MATVEC_MAX_K_F32, PARTS<EF_F32>) <= SMEM_MOST, "one token of the longest rows fits");
 
 struct MatvecArgs {
     int N, K, tokens;

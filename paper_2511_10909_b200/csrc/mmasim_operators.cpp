@@ -213,7 +213,8 @@ int mmasim_matvec4(int w_fmt, int fmt, int64_t T, int64_t N, int64_t K, const vo
     if (!packed4(w_fmt)) { set_error("%s: weights are MXF4_GST or NVF4_GST", call); return MMASIM_ERR_UNSUPPORTED; }
     if (element_fmt(fmt) < 0) { set_error("%s: x and y are FP32, BF16 or FP16", call); return MMASIM_ERR_INVALID_ARG; }
     if (T < 0 || T > 0x7FFFFFFF || N < 1 || N > 0x40000000 || K < 32 || K % 32 || K > (fmt == MMASIM_F32 ? MATVEC_MAX_K_F32 : ROWS_MAX_K)) {
-        set_error("%s: T = %lld, N = %lld, K = %lld: T from 0 on, N from 1 to 2^30 and multiples of 32 up to 32768 (FP32: 28672) for K are taken", call, (long long)T, (long long)N, (long long)K);
+        set_error("%s: T = %lld, N = %lld, K = %lld: T from 0 on, N from 1 to 2^30 and multiples of 32 up to %d (FP32: %d) for K are taken", call, (long long)T, (long long)N, (long long)K,
+                  int(ROWS_MAX_K), int(MATVEC_MAX_K_F32));
         return MMASIM_ERR_SHAPE;
     }
     int st = check_ld(call, "W", &ldw, K);

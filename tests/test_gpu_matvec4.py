@@ -163,6 +163,16 @@ def test_strides_outputs_and_streams():
     assert mmasim.matvec4("mxf4", W, sf[:, ::2].contiguous(), x[:0]).shape == (0, N)
 
 
+@pytest.mark.parametrize("dtype,K", [("fp32", 20480), ("fp32", 20448), ("bf16", 32768), ("fp16", 32736)])
+@pytest.mark.parametrize("fmt", ["mxf4", "nvf4"])
+def test_longest_rows(fmt, dtype, K):
+    """Shared memory then holds few tokens: calls for several read the weights more than once."""
+    codes, sf, rs = layer(40, K, fmt)
+    for T in (1, 2, 3, 7):
+        x = tokens(T, K, dtype)
+        check(mmasim.matvec4(fmt, cuda(ref.pack(codes, fmt)), cuda(sf), x.cuda(), cuda(rs)), x, codes, sf, rs, fmt, dtype)
+
+
 def test_weights_beyond_32_bits():
     """Rows of a matrix whose offsets pass 2^32 bytes."""
     K, N, ld = 64, 3, (1 << 31) + 32                                       # bytes between rows

@@ -11,6 +11,7 @@ from helpers import host_program
 PROGRAM = r"""
 #include <cstdio>
 #include <cstring>
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include "mmasim_internal.h"
 #define SHOWN extern "C" __attribute__((visibility("default")))
@@ -23,6 +24,12 @@ SHOWN cudaError_t cudaPointerGetAttributes(cudaPointerAttributes* a, const void*
     std::memset(a, 0, sizeof(*a));
     a->type = reinterpret_cast<uintptr_t>(p) < 0x10000 ? cudaMemoryTypeUnregistered : cudaMemoryTypeDevice;
     a->device = reinterpret_cast<uintptr_t>(p) >= 0x7000000000 ? 1 : 0;
+    return cudaSuccess;
+}
+static CUresult encode(CUtensorMap*, ...) { return CUDA_SUCCESS; }
+SHOWN cudaError_t cudaGetDriverEntryPoint(const char*, void** f, unsigned long long, cudaDriverEntryPointQueryResult* found) {
+    *f = reinterpret_cast<void*>(encode);
+    *found = cudaDriverEntryPointSuccess;
     return cudaSuccess;
 }
 static char* at(long long x) { return reinterpret_cast<char*>(x); }
@@ -113,6 +120,10 @@ int main() {
     mat("mat_fmt", MMASIM_E4M3, MMASIM_BF16, 1, 16, 64, W, 0, S, RS, X, O);
     mat("mat_type", MMASIM_NVF4_GST, MMASIM_F64, 1, 16, 64, W, 0, S, RS, X, O);
     mat("mat_k", MMASIM_NVF4_GST, MMASIM_BF16, 1, 16, 48, W, 0, S, RS, X, O);
+    mat("mat_k_f32", MMASIM_NVF4_GST, MMASIM_F32, 2, 16, 20480, W, 0, S, RS, X, O);
+    mat("mat_k_f32_more", MMASIM_NVF4_GST, MMASIM_F32, 1, 16, 20512, W, 0, S, RS, X, O);
+    mat("mat_k_most", MMASIM_NVF4_GST, MMASIM_BF16, 3, 16, 32768, W, 0, S, RS, X, O);
+    mat("mat_k_more", MMASIM_NVF4_GST, MMASIM_BF16, 1, 16, 32800, W, 0, S, RS, X, O);
     mat("mat_n", MMASIM_NVF4_GST, MMASIM_BF16, 1, 0, 64, W, 0, S, RS, X, O);
     mat("mat_ld", MMASIM_NVF4_GST, MMASIM_BF16, 1, 16, 64, W, 72, S, RS, X, O);
     mat("mat_align", MMASIM_NVF4_GST, MMASIM_BF16, 1, 16, 64, W + 8, 0, S, RS, X, O);
@@ -130,7 +141,7 @@ WANT = dict(row=OK, mx=OK, nv=OK, no_rows=OK, in_fmt=ARG, out_fmt=UNSUPPORTED, p
             norm_weight_type=ARG, norm_weight_f32=OK, norm_bare=OK, norm_over_weight=ARG, norm_e4m3=OK, norm_e4m3_over_x=ARG, norm_f32_out=UNSUPPORTED,
             norm_plain_scale=ARG, norm_eps=ARG, norm_shifted_rows=ARG, norm_null=ARG, back=OK, back_dx_is_dy=OK, back_dx_is_h=OK, back_dx_shifted=ARG,
             back_small_workspace=ARG, back_no_workspace=ARG, back_no_dweight=OK, back_dweight_over_weight=ARG, back_workspace_over_dx=ARG, back_weight_type=ARG,
-            back_no_h=ARG, back_no_rows=OK, mat=OK, mat_no_scale=OK, mat_no_tokens=OK, mat_fmt=UNSUPPORTED, mat_type=ARG, mat_k=SHAPE, mat_n=SHAPE, mat_ld=ALIGN,
+            back_no_h=ARG, back_no_rows=OK, mat=OK, mat_no_scale=OK, mat_no_tokens=OK, mat_fmt=UNSUPPORTED, mat_type=ARG, mat_k=SHAPE, mat_k_f32=OK, mat_k_f32_more=SHAPE, mat_k_most=OK, mat_k_more=SHAPE, mat_n=SHAPE, mat_ld=ALIGN,
             mat_align=ALIGN, mat_sf_align=ALIGN, mat_sf_bytes=OK, mat_over=ARG, mat_null=ARG)
 
 
