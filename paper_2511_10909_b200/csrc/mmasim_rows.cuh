@@ -7,7 +7,7 @@
 //   blocks of 16 s = max(row's max |y| / 2688, 2^-100), g = nearest UE4M3 of max |y| / 6s, code = nearest(y / gs)     NVF4
 // with FP32 roundings in between, as plain FP32 arithmetic has them (the sum of squares is the one value whose order is the kernel's own).
 //
-// What bounds it is memory: 7 bytes an element for BF16 with a residual into FP8, some 18 instructions.  A row is `threads` threads (8, 16 or
+// What bounds it is memory: 7 bytes an element for BF16 with a residual into FP8.  A row is `threads` threads (8, 16 or
 // 32 of a warp, or a CTA), each with V eights of consecutive elements `threads` eights apart, so that a warp's loads are contiguous and a
 // block of 32 (16) is four (two) neighbouring lanes; the row stays in registers from the load to the codes.
 #pragma once
@@ -232,18 +232,27 @@ __global__ void __launch_bounds__(MAX_THREADS) rows_kernel(const Args a) {
 }
 
 // Threads per row and eights per thread.  Few rows are a matter of latency: the most threads.  Many rows are one of instructions, and what a
-// thread does once a row (the exchanges, the scale) counts less with several eights: a norm takes 256 threads, where its rows need more than
-// four eights of them the fewest that do, quantisation 128.  BF16, 4096 x 4096, us with 512 / 256 / 128 threads: norm into MXFP8 23.5 / 21.1 /
-// 22.2, E4M3 rows 13.7 / 11.0 / 9.9; norm of 16384 x 8192 into E4M3 with 512 / 256 threads 170 / 138.
+// thread does once a row (the exchanges, the scale) counts less with several eights; a row of a warp or less needs no barrier either, and a CTA
+// then has several.  So, where all of a row's accesses are of 16 bytes, a row takes the fewest threads that still give every SM 512:
+//   - with eight eights each where 16-bit rows are quantised with a scale of the row (us, threads per row before and now: E5M2 of 2048 x 14336
+//     448 / 224, 20.7 / 15.7; E4M3 of 32768 x 512 64 / 8, 18.9 / 10.0; NVF4 of 4096 x 14336 448 / 224, 38.0 / 30.0);
+//   - with four else, if the row is a warp's then: larger ones of CTAs of one or two warps gain nothing (MXFP8 of 32768 x 512 64 / 16, 18.6 / 9.3;
+//     norm of 8192 x 2048 into E4M3 256 / 64, 24.8 / 21.7; of 65536 x 128 16 / 8, 8.6 / 6.9), nor do norms of FP32 rows (16384 x 512 64 / 16, 21 / 29).
+// Others of many rows: a norm takes 256 threads, where its rows need more than four eights of them the fewest that do, quantisation 128.  BF16,
+// 4096 x 4096, us with 512 / 256 / 128 threads: norm into MXFP8 23.5 / 21.1 / 22.2; norm of 16384 x 8192 into E4M3 with 512 / 256 threads 170 / 138.
 constexpr int64_t FEW_ROWS = 296;
+constexpr int SHORT_ROW = 256;              // eights
 struct Shape { int threads, v; };
-inline Shape shape(int64_t M, int K, bool norm, bool whole_warps) {
+inline Shape shape(int64_t M, int K, bool norm, int most, bool whole_warps) {           // most: eights per thread where every access is of 16 bytes, else 1
     const int eights = (K + 7) / 8;
-    if (eights <= 8 && !whole_warps) return {8, 1};
-    if (eights <= 16 && !whole_warps) return {16, 1};
-    if (eights <= 32) return {32, 1};
     int v = 1;
-    while (M > FEW_ROWS && v < 4 && eights > v * (norm ? 256 : 128)) v *= 2;
+    if (M > FEW_ROWS && (most == 8 || eights <= SHORT_ROW))
+        while (v < most && eights > v * 8 && M * eights >= 2 * v * 148 * 512) v *= 2;
+    const int threads = (eights + v - 1) / v;
+    if (threads <= 8 && !whole_warps) return {8, v};
+    if (threads <= 16 && !whole_warps) return {16, v};
+    if (threads <= 32) return {32, v};
+    while (most < 8 && M > FEW_ROWS && v < 4 && eights > v * (norm ? 256 : 128)) v *= 2;
     while (eights > v * MAX_THREADS) v *= 2;
     return {((eights + v - 1) / v + 31) / 32 * 32, v};
 }
@@ -263,7 +272,9 @@ cudaError_t launch_out(const Args& a, int v, cudaStream_t stream) {
 template <int T, int OUT>
 cudaError_t launch_out(Args a, bool norm, cudaStream_t stream) {
     const bool vec = a.K % 8 == 0 && a.vec_x && a.vec_o && a.vec_w && (!a.residual || (a.vec_r && a.vec_h));
-    const Shape s = shape(a.M, a.K, norm, !vec && SPREAD_ROWS<OUT, false>);
+    constexpr bool ROW_SCALES = OUT == OUT_FP8 || OUT == OUT_NVF4;
+    const int most = !vec || (norm && T == EF_F32) ? 1 : !norm && ROW_SCALES && T != EF_F32 ? 8 : 4;
+    const Shape s = shape(a.M, a.K, norm, most, !vec && SPREAD_ROWS<OUT, false>);
     a.threads = s.threads;
     a.inverse_k = 1.0f / float(a.K);
     if constexpr (OUT != OUT_PLAIN)

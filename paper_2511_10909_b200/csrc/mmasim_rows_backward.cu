@@ -15,6 +15,7 @@ namespace {
 using namespace quant;
 
 constexpr int MAX_THREADS = 512;
+constexpr int SHORT_ROW = 128;              // eights
 
 struct BackArgs {
     int64_t M;
@@ -45,42 +46,49 @@ __device__ __forceinline__ float2 row_sums(float2 v, int threads, float2* slot) 
     return v;
 }
 
-// The CTA's share of dweight.
+// The CTA's share of dweight; `group_share`: 32 bytes times V a thread of shared memory that nothing else uses any more, where rows are of a
+// warp or less (then the shares of the CTA's groups are put together first).
 template <int V, bool VEC>
 __device__ __forceinline__ void store_shares(const BackArgs& a, const Pair (&dw)[V][4], float* group_share, int per_cta, int t) {
     float* mine = a.part + int64_t(blockIdx.x) * a.K;
-    const bool groups = V == 1 && a.threads <= 32;      // several rows at a time: the groups' shares first
+    const bool groups = a.threads <= 32;
+    const int pitch = a.threads * 8 * V;
+    float* to = groups ? group_share + threadIdx.x / a.threads * pitch : mine;
+    const int K = groups ? pitch : a.K;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
+    for (int j = 0; j < V; ++j) {
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = VEC ? (t + j * a.threads) * 8 + 2 * i : t + (j * 8 + 2 * i) * a.threads, next = VEC ? 1 : a.threads;
-            float even, odd;
-            split(dw[j][i], even, odd);
-            if (groups) {
-                float* to = group_share + threadIdx.x / a.threads * a.threads * 8;
-                to[k] = even;
-                to[k + next] = odd;
-            } else {
-                if (k < a.K) mine[k] = even;
-                if (k + next < a.K) mine[k + next] = odd;
+        for (int i = 0; i < 4; ++i) split(dw[j][i], v[2 * i], v[2 * i + 1]);
+        if constexpr (VEC) {
+            const int k = (t + j * a.threads) * 8;
+            if (k >= K) continue;
+            reinterpret_cast<float4*>(to + k)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(to + k)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = t + (j * 8 + i) * a.threads;
+                if (k < K) to[k] = v[i];
             }
         }
+    }
     if (!groups) return;
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
-        float s = 0.0f;
-        for (int g = 0; g < per_cta; ++g) s += group_share[g * a.threads * 8 + k];
-        mine[k] = s;
+        float sum = 0.0f;
+        for (int g = 0; g < per_cta; ++g) sum += group_share[g * pitch + k];
+        mine[k] = sum;
     }
 }
+
+extern __shared__ __align__(16) unsigned char back_smem[];
 
 // HOLD: dy and h stay in registers between the sums and the results; else they are read again (rows too long for that).
 template <int T, int V, bool HOLD, bool VEC>
 __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a) {
     using E = typename Elem<T>::type;
     __shared__ float2 slots[2][16];
-    __shared__ float group_share[V == 1 ? 8 * 128 : 1];
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
@@ -168,7 +176,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
             else store_spread<T>(static_cast<E*>(a.dx) + row * a.ld_dx + at, o, K - at, a.threads);
         }
     }
-    if (a.part) store_shares<V, VEC>(a, dw, group_share, per_cta, t);
+    if (a.part) store_shares<V, VEC>(a, dw, reinterpret_cast<float*>(back_smem), per_cta, t);
 }
 
 // Both sums of the row's threads with half the exchanges: after the first, one half of a warp has one sum and the other the other.
@@ -190,16 +198,13 @@ __device__ __forceinline__ float2 row_sums_wide(float2 v, int threads, float* sl
 }
 
 // The same for whole eights at multiples of 16 bytes: `depth` rows (2 or 3) of h, dy and dresidual in shared memory, the threads' slots of 16
-// bytes side by side (a thread's own side by side, free of conflicts between banks too, made the copies three times as slow).
+// bytes side by side (a thread's own side by side, free of conflicts between banks too: 4096 x 4096 45 us instead of 34).
 template <int T, int V> constexpr int RING_SLOTS = 3 * V * (Elem<T>::WORDS / 4);
 template <int T, int V>
 __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackArgs a, const int depth) {
     using E = typename Elem<T>::type;
     constexpr int PER = Elem<T>::WORDS / 4, EACH = 16 / sizeof(E);      // slots of an eight, elements of a slot
-    extern __shared__ uint4 ring[];
     __shared__ float slots[2][32];
-    __shared__ float2 few_slots[1];
-    __shared__ float group_share[V == 1 ? 8 * 128 : 1];
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
     const int group = a.threads > 32 ? 0 : threadIdx.x / a.threads, t = a.threads > 32 ? threadIdx.x : threadIdx.x & (a.threads - 1);
@@ -212,7 +217,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
     E* dx = static_cast<E*>(a.dx) + ahead * a.ld_dx + t * 8;
     auto fetch = [&]() {
         if (ahead < a.M) {
-            const uint32_t to = uint32_t(__cvta_generic_to_shared(ring)) + in;
+            const uint32_t to = uint32_t(__cvta_generic_to_shared(back_smem)) + in;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 if ((t + j * a.threads) * 8 >= a.K) continue;
@@ -252,7 +257,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
             Raw<T> r;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(ring) + out + ((which * V + j) * PER + i) * plane);
+                const uint4 q = *reinterpret_cast<const uint4*>(back_smem + out + ((which * V + j) * PER + i) * plane);
                 r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
             }
             return r;
@@ -274,13 +279,13 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         split(squares, sums.x, odd.x);
         split(products, sums.y, odd.y);
         sums = make_float2(sums.x + odd.x, sums.y + odd.y);
-        sums = a.threads >= 32 ? row_sums_wide(sums, a.threads, slots[turn]) : row_sums(sums, a.threads, few_slots);       // (two sets of slots: one barrier a row)
+        sums = a.threads >= 32 ? row_sums_wide(sums, a.threads, slots[turn]) : row_sums(sums, a.threads, nullptr);       // (two sets of slots: one barrier a row)
         const float r = inverse_root(__fmaf_rn(sums.x, a.inverse_k, a.eps));
         const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             if ((t + j * a.threads) * 8 >= K) continue;
-            Pair hv[4], gv[4], o[4];        // (read again: held, they cost a third of the CTAs of an SM their place)
+            Pair hv[4], gv[4], o[4];        // (read again: held, their registers cost CTAs their place, 4096 x 4096 43 us instead of 34)
             widen<T>(take(0, j), hv);
             widen<T>(take(1, j), gv);
 #pragma unroll
@@ -301,30 +306,42 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         out = out + stage == end ? mine : out + stage;
         dx += stride * a.ld_dx;
     }
-    if (a.part) store_shares<V, true>(a, dw, group_share, per_cta, t);
+    if (!a.part) return;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    store_shares<V, true>(a, dw, reinterpret_cast<float*>(back_smem), per_cta, t);
 }
 
-// dweight: 32 columns a CTA, 32 warps over the shares.
-template <int T>
+// dweight: COLS columns a CTA, 1024 / COLS threads over the shares of each.
+template <int T, int COLS>
 __global__ void __launch_bounds__(1024) dweight_kernel(const float* part, int shares, int K, void* dw, int f32) {
-    __shared__ float s[32][32];
+    constexpr int PARTS = 1024 / COLS;
+    __shared__ float s[32][COLS];
     after_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = lane % COLS, k = blockIdx.x * COLS + col;
     float v = 0.0f;
     if (k < K) {
-        for (int g = warp; g < shares; g += 32 * 8) {
+        for (int g = threadIdx.x / COLS; g < shares; g += PARTS * 8) {
             float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = g + 32 * i < shares ? part[int64_t(g + 32 * i) * K + k] : 0.0f;
+            for (int i = 0; i < 8; ++i) p[i] = g + PARTS * i < shares ? part[int64_t(g + PARTS * i) * K + k] : 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v += p[i];
         }
     }
-    s[warp][lane] = v;
-    __syncthreads();
-    if (warp || k >= K) return;
+    auto columns = [&]() {                  // over a warp's lanes of the same column
 #pragma unroll
-    for (int i = 1; i < 32; ++i) v += s[i][lane];
+        for (int o = COLS; o < 32; o *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    };
+    columns();
+    if (lane < COLS) s[warp][lane] = v;
+    __syncthreads();
+    if (warp) return;
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) v += s[lane / COLS * COLS + i][col];
+    columns();
+    if (lane >= COLS || k >= K) return;
     if (f32) static_cast<float*>(dw)[k] = v;
     else if constexpr (T == EF_F32) static_cast<float*>(dw)[k] = v;
     else if constexpr (T == EF_BF16) static_cast<__nv_bfloat16*>(dw)[k] = __float2bfloat16_rn(v);
@@ -337,8 +354,12 @@ BackShape back_shape(int64_t M, int K) {
     const int eights = (K + 7) / 8;
     BackShape s;
     s.v = 1;
-    if (eights <= 32) s.threads = eights <= 8 ? 8 : (eights <= 16 ? 16 : 32);
+    if (K % 8 == 0 && eights <= SHORT_ROW)
+        while (s.v < 4 && eights > s.v * 8 && M * eights >= 2 * s.v * 148 * 256) s.v *= 2;
+    const int threads = (eights + s.v - 1) / s.v;
+    if (threads <= 32) s.threads = threads <= 8 ? 8 : (threads <= 16 ? 16 : 32);
     else {
+        s.v = 1;
         while (s.v < 4 && eights > s.v * 256) s.v *= 2;
         while (eights > s.v * MAX_THREADS) s.v *= 2;
         s.threads = ((eights + s.v - 1) / s.v + 31) / 32 * 32;
@@ -347,7 +368,7 @@ BackShape back_shape(int64_t M, int K) {
     // as many as an SM holds with their rings and registers (BF16 with a residual, CTAs an SM 2 / 3 / 4: 4096 x 4096 32.6 / 41.0 / 36.8 us,
     // 16384 x 8192 174 / 207 / 183; one eight a thread, 16384 x 1024 46.9 / 37.9 / 34.2), but two rows each: their shares are read again
     const int64_t per_cta = s.threads > 32 ? 1 : 128 / s.threads, want = (M + per_cta - 1) / per_cta, few = (want + 1) / 2 < 148 ? 148 : (want + 1) / 2;
-    int64_t most = 148 * (s.v > 1 ? 2 : 4);
+    int64_t most = 148 * (s.v > 1 && s.threads > 32 ? 2 : 4);
     if (most > few) most = few;
     s.ctas = want < most ? want : most;
     return s;
@@ -374,22 +395,30 @@ cudaError_t launch(const BackArgs& a, const BackShape& s, cudaStream_t stream) {
         }
     }
     const dim3 grid{unsigned(s.ctas)};
+    const size_t share = s.threads > 32 ? 0 : size_t(32) * s.v * s.block;
     switch (s.v) {
-        case 1: return enqueue(backward_kernel<T, 1, true, VEC>, grid, s.block, 0, stream, a);
-        case 2: return enqueue(backward_kernel<T, 2, true, VEC>, grid, s.block, 0, stream, a);
-        case 4: return enqueue(backward_kernel<T, 4, T != EF_F32, VEC>, grid, s.block, 0, stream, a);
+        case 1: return enqueue(backward_kernel<T, 1, true, VEC>, grid, s.block, share, stream, a);
+        case 2: return enqueue(backward_kernel<T, 2, true, VEC>, grid, s.block, share, stream, a);
+        case 4: return enqueue(backward_kernel<T, 4, T != EF_F32, VEC>, grid, s.block, share, stream, a);
         default: return enqueue(backward_kernel<T, 8, false, VEC>, grid, s.block, 0, stream, a);
     }
 }
 template <int T>
-cudaError_t launch(BackArgs a, const BackShape& s, void* dweight, cudaStream_t stream) {
+cudaError_t launch(BackArgs a, BackShape s, void* dweight, cudaStream_t stream) {
     a.threads = s.threads;
     a.inverse_k = 1.0f / float(a.K);
     const bool vec = a.K % 8 == 0 && a.vec_dy && a.vec_h && a.vec_dx && a.vec_w && (!a.dres || a.vec_res);
+    if (vec) {                              // no more than have room for two rows of the ring
+        const int64_t room = int64_t(RING_MOST / (size_t(2) * 3 * s.v * (Elem<T>::WORDS / 4) * 16 * s.block));
+        if (room && s.ctas > 148 * room) s.ctas = 148 * room;
+    }
     cudaError_t err = cudaSuccess;
     if (s.ctas) err = vec ? launch<T, true>(a, s, stream) : launch<T, false>(a, s, stream);
-    if (err == cudaSuccess && dweight)
-        err = enqueue(dweight_kernel<T>, dim3(unsigned((a.K + 31) / 32)), 1024, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32);
+    if (err == cudaSuccess && dweight) {    // columns a CTA by whether the CTAs of 8 have room at once (us with 8 / 32: K = 128 15.9 / 17.0, 2048 32.2 / 32.8, 4096 34.4 / 32.6)
+        const bool few = a.K <= 8 * 2 * 148;
+        err = few ? enqueue(dweight_kernel<T, 8>, dim3(unsigned((a.K + 7) / 8)), 1024, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32)
+                  : enqueue(dweight_kernel<T, 32>, dim3(unsigned((a.K + 31) / 32)), 1024, 0, stream, a.part, int(s.ctas), a.K, dweight, a.w_f32);
+    }
     return err;
 }
 }  // namespace

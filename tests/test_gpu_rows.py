@@ -232,6 +232,25 @@ def test_strides_and_alignment(fmt, lead, off):
         check_backward(d1, w1, dy, h, w, res, dtype, float(np.float32(1e-6)))
 
 
+@pytest.mark.parametrize("M,K", [(16001, 96), (9500, 128), (3001, 512), (1300, 1000), (2500, 1024), (2400, 2048), (700, 4096), (310, 14336)])
+@pytest.mark.parametrize("dtype", list(ref.DTYPES))
+def test_many_rows(dtype, M, K):
+    """Rows of few threads with several eights each, from addresses that 16-byte accesses fit and from others; the last CTA has rows to spare."""
+    x, res, w, h = norm_case(M, K, dtype, True, True)
+    for fmt in ref.FORMATS:
+        if K % 32 == 0 or fmt not in ("mxf4", "nvf4"):
+            q = mmasim.quantize(x.cuda(), fmt)
+            assert_same(q, ref.quantize(x.float().numpy(), fmt), fmt)
+            assert all(a is b or torch.equal(a, b) for a, b in zip(q, mmasim.quantize(strided(x, 3, 1), fmt)))
+    for fmt in [None, "e5m2", "mxe4m3"] + ["nvf4"] * (K % 32 == 0):
+        y, got = mmasim.rms_norm(x.cuda(), w.cuda(), res.cuda(), fmt=fmt)
+        check_norm(y, got, x, res, w, h, dtype, fmt, float(np.float32(1e-6)))
+    dy = rows(M, K, dtype, 3, 0.1)
+    for move in (lambda t: t.cuda(), lambda t: strided(t, 3, 1)):
+        dx, dw = mmasim.rms_norm_backward(move(dy), move(h), w.cuda(), move(res))
+        check_backward(dx, dw, dy, h, w, res, dtype, float(np.float32(1e-6)))
+
+
 def test_rows_far_apart():
     """Offsets beyond 2^32 bytes and 2^31 elements."""
     K, ld = 64, (1 << 30) + 8
