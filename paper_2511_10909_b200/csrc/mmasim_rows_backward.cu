@@ -48,7 +48,7 @@ __device__ __forceinline__ float2 row_sums(float2 v, int threads, float2* slot) 
 
 // The CTA's share of dweight; `group_share`: 32 bytes times V a thread of shared memory that nothing else uses any more, where rows are of a
 // warp or less (then the shares of the CTA's groups are put together first).
-template <int V, bool VEC>
+template <int V, bool VEC, int PER = 1>
 __device__ __forceinline__ void store_shares(const BackArgs& a, const Pair (&dw)[V][4], float* group_share, int per_cta, int t) {
     float* mine = a.part + int64_t(blockIdx.x) * a.K;
     const bool groups = a.threads <= 32;
@@ -61,10 +61,9 @@ __device__ __forceinline__ void store_shares(const BackArgs& a, const Pair (&dw)
 #pragma unroll
         for (int i = 0; i < 4; ++i) split(dw[j][i], v[2 * i], v[2 * i + 1]);
         if constexpr (VEC) {
-            const int k = (t + j * a.threads) * 8;
-            if (k >= K) continue;
-            reinterpret_cast<float4*>(to + k)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(to + k)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            const int k = (t + j * PER * a.threads) * (8 / PER), next = PER == 1 ? 4 : a.threads * 4;
+            if (k < K) *reinterpret_cast<float4*>(to + k) = make_float4(v[0], v[1], v[2], v[3]);
+            if (k + next < K) *reinterpret_cast<float4*>(to + k + next) = make_float4(v[4], v[5], v[6], v[7]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -203,7 +202,9 @@ template <int T, int V> constexpr int RING_SLOTS = 3 * V * (Elem<T>::WORDS / 4);
 template <int T, int V>
 __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackArgs a, const int depth) {
     using E = typename Elem<T>::type;
-    constexpr int PER = Elem<T>::WORDS / 4, EACH = 16 / sizeof(E);      // slots of an eight, elements of a slot
+    // slots of an eight, elements of a slot; slots lie a row's threads apart, so that neighbouring threads copy and store neighbouring 16 bytes
+    // (an FP32 eight in one piece: half of every sector at a time, 4096 x 4096 68.8 us instead of 47.0)
+    constexpr int PER = Elem<T>::WORDS / 4, EACH = 16 / sizeof(E);
     __shared__ float slots[2][32];
     after_previous();
     const int per_cta = a.threads > 32 ? 1 : int(blockDim.x) / a.threads;
@@ -212,22 +213,19 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
     const uint32_t plane = blockDim.x * 16, stage = plane * RING_SLOTS<T, V>, mine = threadIdx.x * 16, end = mine + depth * stage;
     uint32_t in = mine, out = mine;                     // of the row to be fetched and to be read next
     int64_t ahead = int64_t(blockIdx.x) * per_cta + group;
-    const E *dy = static_cast<const E*>(a.dy) + ahead * a.ld_dy + t * 8, *h_at = static_cast<const E*>(a.h) + ahead * a.ld_h + t * 8;
-    const E* res_at = a.dres ? static_cast<const E*>(a.dres) + ahead * a.ld_res + t * 8 : nullptr;
-    E* dx = static_cast<E*>(a.dx) + ahead * a.ld_dx + t * 8;
+    const E *dy = static_cast<const E*>(a.dy) + ahead * a.ld_dy + t * EACH, *h_at = static_cast<const E*>(a.h) + ahead * a.ld_h + t * EACH;
+    const E* res_at = a.dres ? static_cast<const E*>(a.dres) + ahead * a.ld_res + t * EACH : nullptr;
+    E* dx = static_cast<E*>(a.dx) + ahead * a.ld_dx + t * EACH;
     auto fetch = [&]() {
         if (ahead < a.M) {
             const uint32_t to = uint32_t(__cvta_generic_to_shared(back_smem)) + in;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if ((t + j * a.threads) * 8 >= a.K) continue;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int at = j * a.threads * 8 + i * EACH, slot = j * PER + i;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + slot * plane), "l"(h_at + at) : "memory");
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V * PER + slot) * plane), "l"(dy + at) : "memory");
-                    if (a.dres) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (2 * V * PER + slot) * plane), "l"(res_at + at) : "memory");
-                }
+            for (int slot = 0; slot < V * PER; ++slot) {
+                const int at = slot * a.threads * EACH;
+                if (at + t * EACH >= a.K) continue;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + slot * plane), "l"(h_at + at) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V * PER + slot) * plane), "l"(dy + at) : "memory");
+                if (a.dres) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (2 * V * PER + slot) * plane), "l"(res_at + at) : "memory");
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -242,8 +240,18 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
     Pair w[V][4], dw[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int at = (t + j * a.threads) * 8;
-        load_weight8<T, true>(a.w, a.w_f32, at, a.K - at, true, w[j]);
+        if constexpr (PER == 1) {
+            const int at = (t + j * a.threads) * 8;
+            load_weight8<T, true>(a.w, a.w_f32, at, a.K - at, true, w[j]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = ((j * PER + i) * a.threads + t) * EACH;
+                const float4 q = a.w && at < a.K ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + at) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                w[j][2 * i] = pair(q.x, q.y);
+                w[j][2 * i + 1] = pair(q.z, q.w);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) dw[j][i] = 0;
     }
@@ -253,11 +261,13 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         fetch();
         if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else asm volatile("cp.async.wait_group 1;" ::: "memory");
-        auto take = [&](int which, int j) {
+        auto there = [&](int slot) { return (slot * a.threads + t) * EACH < K; };
+        auto take = [&](int which, int j) {             // (zeros where there is nothing)
             Raw<T> r;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint4 q = *reinterpret_cast<const uint4*>(back_smem + out + ((which * V + j) * PER + i) * plane);
+                uint4 q = make_uint4(0, 0, 0, 0);
+                if (PER == 1 || there(j * PER + i)) q = *reinterpret_cast<const uint4*>(back_smem + out + ((which * V + j) * PER + i) * plane);
                 r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
             }
             return r;
@@ -265,7 +275,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         Pair squares = 0, products = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if ((t + j * a.threads) * 8 >= K) continue;
+            if (!there(j * PER)) continue;
             Pair hv[4], gv[4];
             widen<T>(take(0, j), hv);
             widen<T>(take(1, j), gv);
@@ -284,7 +294,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if ((t + j * a.threads) * 8 >= K) continue;
+            if (!there(j * PER)) continue;
             Pair hv[4], gv[4], o[4];        // (read again: held, their registers cost CTAs their place, 4096 x 4096 43 us instead of 34)
             widen<T>(take(0, j), hv);
             widen<T>(take(1, j), gv);
@@ -301,7 +311,10 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
             }
             Raw<T> raw;
             narrow<T>(o, raw);
-            store8<T, true>(dx + j * a.threads * 8, raw, 8, true);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (there(j * PER + i))
+                    *reinterpret_cast<uint4*>(dx + (j * PER + i) * a.threads * EACH) = make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]);
         }
         out = out + stage == end ? mine : out + stage;
         dx += stride * a.ld_dx;
@@ -309,7 +322,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
     if (!a.part) return;
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    store_shares<V, true>(a, dw, reinterpret_cast<float*>(back_smem), per_cta, t);
+    store_shares<V, true, PER>(a, dw, reinterpret_cast<float*>(back_smem), per_cta, t);
 }
 
 // dweight: COLS columns a CTA, 1024 / COLS threads over the shares of each.
