@@ -50,7 +50,7 @@ def _py_ext_cmd() -> list[str]:
            sysconfig.get_paths()["include"]]
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
             f'-DMMASIM_BUILT_AGAINST="{built_against()}"', *(f"-I{d}" for d in inc), os.path.join(CSRC, "mmasim_py.cpp"), "-o", PY_EXT, "-L" + os.path.join(root, "lib"),
-            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

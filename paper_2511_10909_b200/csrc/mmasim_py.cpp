@@ -4,6 +4,7 @@
 // types and strides, a status other than OK): the Python code then does it, and names what is wrong.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include "../../include/mmasim.h"
@@ -155,6 +156,8 @@ PyObject* dot_batch(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- the operators on rows ----
+// A new tensor straight from the allocator: by way of the dispatcher one takes 1.1 us, not 0.8 (with its end), and a norm into FP8 makes three.
+at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, at::Device dev) { return at::Tensor(at::detail::empty_cuda(shape, type, dev, std::nullopt)); }
 int row_fmt(const at::Tensor& t) {
     const at::ScalarType s = t.scalar_type();
     return s == at::kFloat ? MMASIM_F32 : s == at::kBFloat16 ? MMASIM_BF16 : s == at::kHalf ? MMASIM_F16 : -1;
@@ -197,11 +200,10 @@ struct Codes {
         for (int i = 0; i < 3; ++i) {
             if (!given(a[i], &t[i]) || (t[i] && !want[i]) || (a[0] != Py_None && want[i] && !t[i]) || (a[0] == Py_None && t[i])) return false;
         }
-        const at::TensorOptions bytes = at::TensorOptions().dtype(at::kByte).device(dev);
         if (!t[0]) {
-            fresh[0] = at::empty({M, K / per_byte}, bytes);
-            if (want[1]) fresh[1] = at::empty({M, (K + block - 1) / block}, bytes);
-            if (want[2]) fresh[2] = at::empty({M}, bytes.dtype(at::kFloat));
+            fresh[0] = empty({M, K / per_byte}, at::kByte, dev);
+            if (want[1]) fresh[1] = empty({M, (K + block - 1) / block}, at::kByte, dev);
+            if (want[2]) fresh[2] = empty({M}, at::kFloat, dev);
             for (int i = 0; i < 3; ++i) if (want[i]) t[i] = &fresh[i];
         }
         ld = rows_ld(t[0], M, K / per_byte, at::kByte, dev) * per_byte;
@@ -266,13 +268,13 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor fresh_out, fresh_res;
         Codes c;
         if (res) {
-            if (!res_out) { fresh_res = at::empty({M, K}, x->options()); res_out = &fresh_res; }
+            if (!res_out) { fresh_res = empty({M, K}, type, dev); res_out = &fresh_res; }
             if ((p.ld_residual = rows_ld(res, M, K, type, dev)) < 1 || (p.ld_residual_out = rows_ld(res_out, M, K, type, dev)) < 1) Py_RETURN_NONE;
             p.residual = res->data_ptr();
             p.residual_out = res_out->data_ptr();
         }
         if (fmt == -2) {
-            if (!out) { fresh_out = at::empty({M, K}, x->options()); out = &fresh_out; }
+            if (!out) { fresh_out = empty({M, K}, type, dev); out = &fresh_out; }
             if ((p.ld_out = rows_ld(out, M, K, type, dev)) < 1) Py_RETURN_NONE;
             p.out = out->data_ptr();
             p.out_fmt = in;
@@ -323,12 +325,12 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     try {
         const c10::cuda::OptionalCUDAGuard guard(dev);
         at::Tensor fresh_dx, dweight, workspace;
-        if (!dx) { fresh_dx = at::empty({M, K}, h->options()); dx = &fresh_dx; }
+        if (!dx) { fresh_dx = empty({M, K}, type, dev); dx = &fresh_dx; }
         if ((p.ld_dx = rows_ld(dx, M, K, type, dev)) < 1) Py_RETURN_NONE;
         if (need) {
-            dweight = at::empty({K}, w ? w->options() : h->options());
+            dweight = empty({K}, w ? w->scalar_type() : type, dev);
             p.workspace_bytes = p_workspace(M, K);
-            workspace = at::empty({int64_t(p.workspace_bytes)}, h->options().dtype(at::kByte));
+            workspace = empty({int64_t(p.workspace_bytes)}, at::kByte, dev);
             p.dweight = dweight.data_ptr();
             p.workspace = workspace.data_ptr();
         }
@@ -368,7 +370,7 @@ PyObject* matvec4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     try {
         const c10::cuda::OptionalCUDAGuard guard(dev);
         at::Tensor fresh;
-        if (!out) { fresh = at::empty({T, N}, x->options()); out = &fresh; }
+        if (!out) { fresh = empty({T, N}, x->scalar_type(), dev); out = &fresh; }
         const int64_t ldy = rows_ld(out, T, N, x->scalar_type(), dev);
         if (ldy < 1) Py_RETURN_NONE;
         const void *w = W->data_ptr(), *s_ptr = sf->data_ptr(), *x_ptr = x->data_ptr();
