@@ -21,7 +21,7 @@
 // how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next three steps in flight
 // into its own part of shared memory, over the ends of tiles too (28672 x 8192: 49 us with these asynchronous copies where loads into registers,
 // as far ahead, took 66).
-// Where it ends: 28672 x 8192 NVFP4, one token, 30.3 us, 0.67 of the copy rate (the copies alone 25.9: 2.5 us until x is staged and the first
+// Where it ends: 28672 x 8192 NVFP4, one token, 29.4 us, 0.69 of the copy rate (the copies alone 25.7: 2.5 us until x is staged and the first
 // tile begun, 7 % for tiles that do not fill the last round; then 2.6 instructions per clock and scheduler quarter).
 #include <type_traits>
 #include "mmasim_quant.cuh"
@@ -543,8 +543,9 @@ struct Kernel {
         __syncwarp();
     }
 
-    // x into its columns: a warp takes a step of a token at a time, 16 of its threads the 128 elements that share a scale.  The next ones are
-    // on their way meanwhile.  Whether all of it is exact in FP16.
+    // x into its columns: a warp takes a step of a token at a time, 16 of its threads the 128 elements that share a scale.  The next two
+    // are on their way meanwhile, asked for in front of the weights (28672 x 8192: 29.4 us, 30.0 with one; not at all where there are none, 4096 x
+    // 4096 6.1 instead of 6.5).  Whether all of it is exact in FP16.
     static constexpr int BATCH = BLOCKS || T == EF_F32 ? 1 : 4;           // (more of few: more code to be fetched than there is to do)
     struct Steps {
         Raw<T> raw[BATCH];
@@ -563,13 +564,17 @@ struct Kernel {
             step += WARPS;
         }
     }
-    __device__ __forceinline__ bool stage(Steps& s) {
+    __device__ __forceinline__ void ask_behind(const Steps& s, Steps& following) const {
+        following.tok = s.tok;
+        following.step = s.step + BATCH * WARPS;
+        ask(following);
+    }
+    __device__ __forceinline__ bool stage(Steps& s, Steps& next) {
         bool exact = true;
         while (s.tok < a.tokens) {
             Steps following;
-            following.tok = s.tok;
-            following.step = s.step + BATCH * WARPS;
-            ask(following);
+            following.tok = a.tokens;
+            if (next.tok < a.tokens) ask_behind(next, following);
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
                 if (s.tok < a.tokens) {
@@ -583,7 +588,8 @@ struct Kernel {
                     s.settle(l.steps);
                 }
             }
-            s = following;
+            s = next;
+            next = following;
         }
         return exact;
     }
@@ -724,19 +730,23 @@ __global__ void __launch_bounds__(WARPS * 32, 1) matvec4_kernel(const MatvecArgs
     after_previous();
     Kernel<T, NV, NT, BLOCKS> k(a);
     // x is asked for before the weights' stream begins, and staged before more than a step a warp of it is in front.
-    typename Kernel<T, NV, NT, BLOCKS>::Steps steps;
+    typename Kernel<T, NV, NT, BLOCKS>::Steps steps, next;
     steps.tok = 0;
     steps.step = k.warp;
     const bool as_it_is = T == EF_F16 && a.vec_x;
     if (as_it_is) k.copy_x(steps);
-    else k.ask(steps);
+    else {
+        k.ask(steps);
+        next.tok = a.tokens;
+        if (a.tokens * a.l.steps > k.BATCH * WARPS) k.ask_behind(steps, next);
+    }
     const bool plain = a.K % STEP == 0 && a.copy_codes;
     if (plain) k.template fetch<false>();
     else k.template fetch<true>();
     if (BLOCKS && threadIdx.x < 2 * HALF_BYTES / 4) reinterpret_cast<uint32_t*>(smem + a.l.zeros)[threadIdx.x] = 0u;
     bool exact = true;
     if (as_it_is) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else exact = k.stage(steps);
+    else exact = k.stage(steps, next);
     const bool wide = __syncthreads_or(!exact);
     for (int i = 2; i < a.stages; ++i) {
         if (plain) k.template fetch<false>();
