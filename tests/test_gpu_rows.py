@@ -80,6 +80,16 @@ def test_quantize_extremes(fmt):
     assert_same(mmasim.quantize(x.cuda(), fmt), ref.quantize(x.numpy(), fmt), fmt)
 
 
+@pytest.mark.parametrize("dtype", list(ref.DTYPES))
+@pytest.mark.parametrize("fmt", ref.FORMATS)
+def test_zeros_keep_their_signs(fmt, dtype):
+    for M, K in [(40, 96), (3, 4096), (7, 1000 if fmt not in ("mxf4", "nvf4") else 992)]:
+        x = rows(M, K, dtype, 2)
+        x[:, ::5] = 0.0
+        x[:, 1::7] = -0.0
+        assert_same(mmasim.quantize(x.cuda(), fmt), ref.quantize(x.float().numpy(), fmt), fmt)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2", "nvf4"])
 def test_quotients_are_rounded_as_division_rounds_them(fmt):
     """Rows around the codes' ties: quotients next to one differ in their last bits."""
