@@ -672,6 +672,7 @@ struct Kernel {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) product.acc[nt][0] = product.acc[nt][1] = product.acc[nt][2] = product.acc[nt][3] = 0.0f;
         while (now.done < tiles) {
+            __syncwarp();                               // (the codes of a stage are read by other lanes than copied them: all have read before it is filled again)
             fetch<GENERAL>();
             await();
             const int step = now.step();
