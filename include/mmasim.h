@@ -291,7 +291,7 @@ typedef struct {
 int mmasim_rms_norm(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_args* args, void* stream);
 
 /* Its gradients, a quantised output taken as if it were not (straight through).  With r = 1 / sqrt(mean of h^2 + eps) and g = dy * weight:
- *   dx = r g - h (r^3 / K) sum(g h) + dresidual     the gradient of x and of residual alike, one rounding to the rows' type
+ *   dx = r (g - (h r) (r / K) sum(g h)) + dresidual     the gradient of x and of residual alike, one rounding to the rows' type
  *   dweight = sum over the rows of dy h r           one rounding to weight_fmt; zeros for M = 0
  * h is what the forward pass stored (residual_out, or x).  dweight is the same from run to run: the rows are added in a fixed order, through
  * `workspace` (device, mmasim_rms_norm_backward_workspace(M, K) bytes, 16-byte aligned; not needed without dweight), whose contents before

@@ -1,7 +1,9 @@
 // Gradients of the root-mean-square norm (mmasim_rms_norm_backward).  With r = 1 / sqrt(mean h^2 + eps) and g = dy w, by row:
 //
-//   dx = r g - h (r^3 / K) sum(g h) + dresidual         dweight = sum over rows of dy h r
+//   dx = r (g - (h r) m) + dresidual,  m = (r / K) sum(g h)         dweight = sum over rows of dy (h r)
 //
+// (In this order no factor leaves FP32 that dx does not: h r is of size one, m of g's.  r^3, of which the formula is often written, is subnormal
+// for rows from 4e12 on, zero from 1e15 on, and infinite for those below 1e-13 where eps is 0.)
 // One pass: both sums of a row (h^2 and g h) come from the same loads, so nothing of the forward pass has to be kept but h.  Memory is what
 // bounds it (8 bytes an element in BF16 with a residual).  A CTA walks over rows, a thread keeps its columns and with them its share of
 // dweight in registers; the CTAs' shares go to the workspace, and a second kernel adds them column by column, in one order whatever runs first.
@@ -144,7 +146,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
         split(products, sums.y, odd.y);
         sums = row_sums(make_float2(sums.x + odd.x, sums.y + odd.y), a.threads, slots[turn]);          // (two sets of slots: one barrier a row)
         const float r = inverse_root(__fmaf_rn(sums.x, a.inverse_k, a.eps));
-        const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
+        const Pair rr = both(r), m = both(-__fmul_rn(__fmul_rn(r, sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int at = place(j);
@@ -160,8 +162,9 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_kernel(const BackArgs a)
             weight(at, K, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                dw[j][i] = fma2(g[i], mul2(hv[i], rr), dw[j][i]);
-                out[i] = fma2(mul2(g[i], w[i]), rr, mul2(hv[i], c));
+                const Pair unit = mul2(hv[i], rr);
+                dw[j][i] = fma2(g[i], unit, dw[j][i]);
+                out[i] = mul2(fma2(unit, m, mul2(g[i], w[i])), rr);
             }
             if (a.dres) {
                 Pair res[4];
@@ -291,7 +294,7 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
         sums = make_float2(sums.x + odd.x, sums.y + odd.y);
         sums = a.threads >= 32 ? row_sums_wide(sums, a.threads, slots[turn]) : row_sums(sums, a.threads, nullptr);       // (two sets of slots: one barrier a row)
         const float r = inverse_root(__fmaf_rn(sums.x, a.inverse_k, a.eps));
-        const Pair rr = both(r), c = both(-__fmul_rn(__fmul_rn(__fmul_rn(__fmul_rn(r, r), r), sums.y), a.inverse_k));
+        const Pair rr = both(r), m = both(-__fmul_rn(__fmul_rn(r, sums.y), a.inverse_k));
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             if (!there(j * PER)) continue;
@@ -300,8 +303,9 @@ __global__ void __launch_bounds__(MAX_THREADS) backward_ring_kernel(const BackAr
             widen<T>(take(1, j), gv);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                dw[j][i] = fma2(gv[i], mul2(hv[i], rr), dw[j][i]);
-                o[i] = fma2(mul2(gv[i], w[j][i]), rr, mul2(hv[i], c));
+                const Pair unit = mul2(hv[i], rr);
+                dw[j][i] = fma2(gv[i], unit, dw[j][i]);
+                o[i] = mul2(fma2(unit, m, mul2(gv[i], w[j][i])), rr);
             }
             if (a.dres) {
                 Pair res[4];
