@@ -779,11 +779,12 @@ cudaError_t launch(MatvecArgs a, int64_t all, int64_t bytes, cudaStream_t stream
         a.y = const_cast<char*>(y) + done * a.ldy * bytes;
         const int columns = a.tokens * PARTS<T>;
         const bool blocks = PARTS<T> == 1 && a.tokens <= BLOCK_TOKENS;
-        const int nt = blocks ? (a.tokens <= 2 ? 1 : 2) : (columns <= 8 ? 1 : 2);
+        const int nt = blocks || columns <= 8 ? 1 : 2;
         a.stages = layout(a.K, columns, nt, 4, &a.l) <= SMEM_MOST ? 4 : 2;
         const size_t smem = layout(a.K, columns, nt, a.stages, &a.l);
         if constexpr (PARTS<T> == 1) {
-            if (blocks) { err = nt == 1 ? launch<T, NV, 1, true>(a, smem, stream) : launch<T, NV, 2, true>(a, smem, stream); continue; }
+            static_assert(BLOCK_TOKENS * 4 <= 8, "a token by block has four of the instruction's eight columns");
+            if (blocks) { err = launch<T, NV, 1, true>(a, smem, stream); continue; }
         }
         err = nt == 1 ? launch<T, NV, 1, false>(a, smem, stream) : launch<T, NV, 2, false>(a, smem, stream);
     }

@@ -402,22 +402,30 @@ cudaError_t launch_ring(const BackArgs& a, const BackShape& s, cudaStream_t stre
     }
     return enqueue(backward_ring_kernel<T, V>, dim3(unsigned(s.ctas)), s.block, smem, stream, a, depth);
 }
+constexpr size_t two_rows(int words, int v, unsigned block) { return size_t(2) * 3 * v * (words / 4) * 16 * block; }       // of the ring
 template <int T, bool VEC>
 cudaError_t launch(const BackArgs& a, const BackShape& s, cudaStream_t stream) {
-    if constexpr (VEC) {
-        if (size_t(2) * 3 * s.v * (Elem<T>::WORDS / 4) * 16 * s.block <= RING_MOST) {
-            if (s.v == 1) return launch_ring<T, 1>(a, s, stream);
-            if (s.v == 2) return launch_ring<T, 2>(a, s, stream);
-            if (s.v == 4) return launch_ring<T, 4>(a, s, stream);
-        }
-    }
     const dim3 grid{unsigned(s.ctas)};
-    const size_t share = s.threads > 32 ? 0 : size_t(32) * s.v * s.block;
-    switch (s.v) {
-        case 1: return enqueue(backward_kernel<T, 1, true, VEC>, grid, s.block, share, stream, a);
-        case 2: return enqueue(backward_kernel<T, 2, true, VEC>, grid, s.block, share, stream, a);
-        case 4: return enqueue(backward_kernel<T, 4, T != EF_F32, VEC>, grid, s.block, share, stream, a);
-        default: return enqueue(backward_kernel<T, 8, false, VEC>, grid, s.block, 0, stream, a);
+    if constexpr (VEC) {
+        constexpr int WORDS = Elem<T>::WORDS;
+        static_assert(two_rows(WORDS, 2, MAX_THREADS) <= RING_MOST && (T == EF_F32 || two_rows(WORDS, 4, MAX_THREADS) <= RING_MOST),
+                      "the ring holds two rows of all threads but of four eights each in FP32, and of eight");
+        if (s.v == 1) return launch_ring<T, 1>(a, s, stream);
+        if (s.v == 2) return launch_ring<T, 2>(a, s, stream);
+        if (s.v == 4) {
+            if constexpr (T == EF_F32)
+                if (two_rows(WORDS, 4, s.block) > RING_MOST) return enqueue(backward_kernel<T, 4, false, true>, grid, s.block, 0, stream, a);
+            return launch_ring<T, 4>(a, s, stream);
+        }
+        return enqueue(backward_kernel<T, 8, false, true>, grid, s.block, 0, stream, a);
+    } else {
+        const size_t share = s.threads > 32 ? 0 : size_t(32) * s.v * s.block;
+        switch (s.v) {
+            case 1: return enqueue(backward_kernel<T, 1, true, false>, grid, s.block, share, stream, a);
+            case 2: return enqueue(backward_kernel<T, 2, true, false>, grid, s.block, share, stream, a);
+            case 4: return enqueue(backward_kernel<T, 4, T != EF_F32, false>, grid, s.block, share, stream, a);
+            default: return enqueue(backward_kernel<T, 8, false, false>, grid, s.block, 0, stream, a);
+        }
     }
 }
 template <int T>
@@ -426,7 +434,7 @@ cudaError_t launch(BackArgs a, BackShape s, void* dweight, cudaStream_t stream) 
     a.inverse_k = 1.0f / float(a.K);
     const bool vec = a.K % 8 == 0 && a.vec_dy && a.vec_h && a.vec_dx && a.vec_w && (!a.dres || a.vec_res);
     if (vec) {                              // no more than have room for two rows of the ring
-        const int64_t room = int64_t(RING_MOST / (size_t(2) * 3 * s.v * (Elem<T>::WORDS / 4) * 16 * s.block));
+        const int64_t room = int64_t(RING_MOST / two_rows(Elem<T>::WORDS, s.v, s.block));
         if (room && s.ctas > 148 * room) s.ctas = 148 * room;
     }
     cudaError_t err = cudaSuccess;
