@@ -170,7 +170,10 @@ template <int T> __device__ __forceinline__ uint32_t largest_of(uint32_t m) {
 }
 // x / t as the product with the reciprocal, corrected by its exact remainder (Markstein, Computation of elementary functions on the IBM RISC
 // System/6000, 1990): a quotient that is an FP32 number comes out exactly, so that ties of the codes stay ties, every other one as division
-// rounds it unless it lies within 2^-21 of a unit in the last place from the middle of two numbers.  For t in 2^-60 .. 2^126, where the
+// rounds it unless it lies within 2^-21 of a unit in the last place from the middle of two numbers.  No code changes with those: only where one of
+// the two numbers is a tie of the codes could one, such divisors and dividends are few (a tie has at most four bits behind the leading one), and
+// with a reciprocal known to a unit the only pair of them to come out otherwise has a divisor of 24 ones, for which it does not either
+// (tests/test_gpu_quotients.py goes through them all).  For t in 2^-60 .. 2^126, where the
 // remainder of a quotient that no format rounds to zero (2^-18 and up) is exact and the reciprocal normal; below, CUDA's division.
 // A remainder of nothing is -0 (rounding down; it is exact otherwise), which leaves a quotient of zero its sign.
 // (Its reciprocal and a second correction, exact for every quotient, made NVFP4 4096 x 4096 14.8 us where it took 13.4 without.)
