@@ -5,6 +5,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include "../../include/mmasim.h"
@@ -176,6 +177,8 @@ bool given(PyObject* o, const at::Tensor** t) {         // false: something else
     *t = o == Py_None ? nullptr : tensor(o);
     return o == Py_None || *t;
 }
+// Autograd would be asked for a gradient through it, and no call records one.
+bool traced(const at::Tensor* t) { return t && t->requires_grad() && c10::GradMode::is_enabled(); }
 PyObject* result(PyObject* given_one, const at::Tensor& fresh, bool any) {      // a new reference
     if (given_one != Py_None) { Py_INCREF(given_one); return given_one; }
     if (any) return THPVariable_Wrap(fresh);
@@ -263,6 +266,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     mmasim_rms_norm_args p = {};
     const int in = row_fmt(*x);
     if (in < 0 || K < 1 || (p.ldx = rows_ld(x, M, K, type, dev)) < 1 || !weight_of(a[1], K, *x, in, &w, &p.weight_fmt)) Py_RETURN_NONE;
+    if ((fmt == -2 || res) && (traced(x) || traced(res) || (fmt == -2 && traced(w)))) Py_RETURN_NONE;
     try {
         const c10::cuda::OptionalCUDAGuard guard(dev);
         at::Tensor fresh_out, fresh_res;
@@ -367,6 +371,7 @@ PyObject* matvec4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (in < 0 || K < 1 || K % 32 || N < 1) Py_RETURN_NONE;
     const int64_t ldx = rows_ld(x, T, K, x->scalar_type(), dev), ldw = rows_ld(W, N, K / 2, at::kByte, dev) * 2;
     if (ldx < 1 || ldw < 1 || !packed(sf, {N, K / block}, at::kByte, dev) || (rs && !packed(rs, {N}, at::kFloat, dev))) Py_RETURN_NONE;
+    if (traced(x) || traced(rs)) Py_RETURN_NONE;
     try {
         const c10::cuda::OptionalCUDAGuard guard(dev);
         at::Tensor fresh;

@@ -112,6 +112,7 @@ def quantised_layer(x, gain, W, rows=(("hopper", "e4m3"), ("blackwell", "e4m3"),
                    unquantised product.
     x, residual: tokens x K, W: N x K, of one type (FP32, BF16, FP16); gain: K."""
     import torch
+    x, gain, W, residual = (t if t is None else t.detach() for t in (x, gain, W, residual))
     fp64 = mmasim.Model("ampere", "fp64", "fp64")
     product = lambda a, b: mmasim.gemm(fp64, a.contiguous().view(torch.int64), b.contiguous().view(torch.int64)).view(torch.float64)
     y, h = mmasim.rms_norm(x, gain, residual, eps=eps)

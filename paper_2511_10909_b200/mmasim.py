@@ -559,6 +559,13 @@ def _row_matrix(x, name):
     return x.shape[0], x.shape[1], x.device, _row_format(x, name)
 
 
+def _untraced(call, *tensors):
+    """Refuses inputs whose gradient autograd would be asked for: no call records one."""
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise MmasimError(1, f"{call} records nothing for autograd, and an input requires a gradient: call it under torch.no_grad()")
+
+
 def _packed_vector(t, name, shape, dtype, device):
     if not t.is_cuda or t.device != device or t.dtype != dtype:
         raise MmasimError(1, f"{name} must be a {dtype} CUDA tensor on {device}")
@@ -620,7 +627,8 @@ def quantize(x, fmt: str, out: Quantized | None = None, *, stream=None) -> Quant
 def rms_norm(x, weight=None, residual=None, *, eps: float = 1e-6, fmt: str | None = None, residual_out=None, out=None, stream=None):
     """Root-mean-square norm of the rows of ``x`` (mmasim_rms_norm): h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight.
     Returns (y, h): y in x's type, or a Quantized of ``fmt``; h is None without a residual.  ``residual_out`` and ``out`` (a tensor, or a
-    Quantized) are written to if given; residual_out may be x or residual, an ``out`` in x's type too.  The weight is of x's type or FP32."""
+    Quantized) are written to if given; residual_out may be x or residual, an ``out`` in x's type too.  The weight is of x's type or FP32.
+    Nothing is recorded for autograd (rms_norm_backward gives the gradients): where y or h would have to carry one, the call is refused."""
     if stream is None:
         quantised = fmt is not None
         bufs = (out if quantised and out is not None else (None, None, None)) if quantised else (out, None, None)
@@ -631,6 +639,7 @@ def rms_norm(x, weight=None, residual=None, *, eps: float = 1e-6, fmt: str | Non
     M, K, dev, x_fmt = _row_matrix(x, "x")
     a = _RmsNormArgs(eps=eps, out_fmt=x_fmt, x=x.data_ptr(), ldx=_rows(x, "x", M, K, x.dtype, dev), weight_fmt=_weight_format(weight, "weight", K, x_fmt, x, dev))
     a.weight = None if weight is None else weight.data_ptr()
+    _untraced("rms_norm", *((x, weight, residual) if fmt is None else () if residual is None else (x, residual)))
     if residual_out is not None and residual is None:
         raise MmasimError(1, "residual_out without a residual")
     with _launching(dev, stream) as s:
@@ -682,7 +691,8 @@ def rms_norm_backward(dy, h, weight=None, dresidual=None, *, eps: float = 1e-6, 
 
 def matvec4(fmt: str, W, sf, x, row_scale=None, *, out=None, stream=None):
     """y = x W^T for a few tokens ``x`` (T x K; FP32, BF16 or FP16) and 4-bit weights ``W`` (N x K / 2 bytes, "mxf4" or "nvf4") with their
-    scales ``sf`` and, where they have them, ``row_scale``, as quantize lays them out (mmasim_matvec4): T x N of x's type, sums in FP32."""
+    scales ``sf`` and, where they have them, ``row_scale``, as quantize lays them out (mmasim_matvec4): T x N of x's type, sums in FP32.
+    Nothing is recorded for autograd: an x or row_scale that requires a gradient is refused unless under torch.no_grad()."""
     if stream is None:
         y = (_fast or _load_fast()).matvec4(FMT.get(fmt, -1), W, sf, x, row_scale, out)
         if y is not None:
@@ -700,6 +710,7 @@ def matvec4(fmt: str, W, sf, x, row_scale=None, *, out=None, stream=None):
     _packed_vector(sf, "sf", (N, K // SCALE_BLOCK[fmt]), torch.uint8, dev)
     if row_scale is not None:
         _packed_vector(row_scale, "row_scale", (N,), torch.float32, dev)
+    _untraced("matvec4", x, row_scale)
     with _launching(dev, stream) as s:
         if out is None:
             out = torch.empty((T, N), dtype=x.dtype, device=dev)
