@@ -96,7 +96,10 @@ def dequantised(q: mmasim.Quantized, fmt: str):
     else:
         v = accuracy.widen(fmt[-4:], q.codes)
     if q.sf is not None:
-        sf = q.sf.view(torch.float8_e4m3fn).double() if fmt == "nvf4" else torch.ldexp(torch.ones_like(q.sf, dtype=torch.float64), q.sf.int() - 127)
+        if fmt == "nvf4":                       # (UE4M3: the sign bit is none)
+            sf = (q.sf & 0x7F).view(torch.float8_e4m3fn).double()
+        else:
+            sf = torch.ldexp(torch.ones_like(q.sf, dtype=torch.float64), q.sf.int() - 127).masked_fill(q.sf == 255, float("nan"))
         v = v * sf.repeat_interleave(mmasim.SCALE_BLOCK[fmt], dim=1)[:, :v.shape[1]]
     return v if q.row_scale is None else v * q.row_scale.double()[:, None]
 
