@@ -318,8 +318,8 @@ int mmasim_rms_norm_backward(int fmt, int64_t M, int64_t K, const mmasim_rms_nor
  * w_fmt MMASIM_MXF4_GST or MMASIM_NVF4_GST: W packed two per byte as for mmasim_gemm_ex (16-byte aligned, ldw elements a row, a multiple of 32,
  * 0 = K), sf N x K / 32 E8M0 or N x K / 16 UE4M3 bytes; row_scale N floats or NULL.  fmt: x and y, FP32, BF16 or FP16.  K a multiple of 32.
  * Products of x, code and scale are exact, sums FP32 (over 128 elements by the matrix instruction, which truncates below 2^-24 of the largest
- * term, then by rounded additions in a fixed order), one rounding to the type of y.  Weights of 2^128 and more (E8M0 codes 253 and 254) may
- * come out infinite.  T >= 0; up to 16 tokens of 16 bits or five of FP32 (fewer where K is too long for their place in shared memory) read the
+ * term, an FP16 x below 2^-14 taken for 2^-14 there, then by rounded additions in a fixed order), one rounding to the type of y.  Weights of
+ * 2^128 and more (E8M0 codes 253 and 254) may come out infinite, and then NaN times zeros of x.  T >= 0; up to 16 tokens of 16 bits or five of FP32 (fewer where K is too long for their place in shared memory) read the
  * weights together.  K up to 32768, FP32 20480. */
 int mmasim_matvec4(int w_fmt, int fmt, int64_t T, int64_t N, int64_t K, const void* W, int64_t ldw, const void* sf, const float* row_scale,
                    const void* x, int64_t ldx, void* y, int64_t ldy, void* stream);

@@ -12,9 +12,11 @@
 // 256 elements of 16 rows take a warp 274 instructions the first way (NVFP4, one token) and 337 the second.
 //
 // x is staged once per CTA in shared memory, a column of FP16 numbers per token (FP32: three, each with what the one before left), scaled by a
-// power of two per 128 elements so that the largest is in 2^14 .. 2^15.  Elements of BF16 down to 2^-32 of the largest of their 128 are exact
-// that way, of FP32 to 2^-39.  256 elements of which one is not exact go through BF16 and its wider exponents instead, from x itself (FP32:
-// three parts), with the codes moved to the lowest bits of a BF16 word's exponent - a number 2^-126 times its value.
+// power of two per 128 elements so that the largest is in 2^14 .. 2^15.  Elements down to 2^-28 of the largest of their 128 are normal FP16 numbers
+// that way (smaller ones, as subnormal numbers, the instruction would align as if they were 2^-14, and cut off bits of a sum of such alone), and
+// then exact.  256 elements of which one is neither that nor zero go another way, from x itself: BF16 through the instruction's BF16 form and
+// its wider exponents, with the codes moved to the lowest bits of a BF16 word's exponent - a number 2^-126 times its value; FP32 through plain
+// multiply-adds (three parts in BF16 end at 2^-133, where FP32 elements below 2^-110 have bits that count).
 // The instruction's sums truncate below 2^-24 of their largest term, so they are taken over 128 elements and added up in FP32.
 //
 // One CTA an SM walks over tiles of 16 rows; its warps split K (256 elements in turn) among the 16, 8, 4 or 2 of them that share a tile, by
@@ -131,9 +133,44 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ float power(int code) { return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7FC00000u : uint32_t(code) << 23); }      // of an E8M0 code
 
-// A step that FP16 has not exactly, through BF16: x from memory.  Four sums of the lane, of eight columns.
-template <int T, bool NV>
-__device__ __noinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const typename Elem<T>::type* x, int64_t ldx, int vec_x, int columns, int per_token, int first, int k) {
+// The value of the lowest four bits of c: they are the lowest of an FP32 word's exponent, a number 2^-126 times it.
+__device__ __forceinline__ float code_value(uint32_t c) { return __fmul_rn(__uint_as_float((c & 8u) << 28 | (c & 7u) << 22), 8.50705917e37f); }
+// A step that FP16 has not exactly, x from memory: four sums of the lane, of eight columns.
+// FP32: every lane multiplies its blocks of two rows with the tokens themselves, whose sums go to the columns of their first parts.  Little of it
+// at once: its registers come on top of the kernel's (all eight codes of a word unrolled 6.9 us, not 6.5, for one token of 4096 x 4096 without such steps).
+template <bool NV>
+__device__ __noinline__ float4 wide_sums_f32(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const float* x, int64_t ldx, int tokens, int first, int k) {
+    constexpr int P = PARTS<EF_F32>;
+    float d[4] = {};
+#pragma unroll 1
+    for (int tok = (first + P - 1) / P; tok < tokens && tok * P < first + 8; ++tok) {
+        float sa = 0.0f, sb = 0.0f;
+#pragma unroll 1
+        for (int four = 0; four < 8; ++four) {
+            const int shift = four & 1 ? 16 : 0;
+            uint32_t wa = word_of(va, four >> 1) >> shift, wb = word_of(vb, four >> 1) >> shift;
+            const float fa = NV ? ue4m3_value(ca >> (four & 4 ? 8 : 0) & 0x7Fu) : power(ca), fb = NV ? ue4m3_value(cb >> (four & 4 ? 8 : 0) & 0x7Fu) : power(cb);
+            const Raw<EF_F32> v = load8<EF_F32, false>(x + (k >= 0 ? tok * ldx + k + four * 4 : 0), k >= 0 ? 4 : 0, false);
+#pragma unroll
+            for (int i = 0; i < 4; ++i, wa >>= 4, wb >>= 4) {
+                sa = __fmaf_rn(__uint_as_float(v.w[i]), __fmul_rn(code_value(wa), fa), sa);
+                sb = __fmaf_rn(__uint_as_float(v.w[i]), __fmul_rn(code_value(wb), fb), sb);
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o *= 2) {
+            sa = __fadd_rn(sa, __shfl_xor_sync(0xFFFFFFFFu, sa, o));
+            sb = __fadd_rn(sb, __shfl_xor_sync(0xFFFFFFFFu, sb, o));
+        }
+        const int c = tok * P - first - 2 * int(threadIdx.x & 3);
+        if (c == 0) { d[0] = sa; d[2] = sb; }
+        if (c == 1) { d[1] = sa; d[3] = sb; }
+    }
+    return make_float4(d[0], d[1], d[2], d[3]);
+}
+// BF16, through the instruction.
+template <bool NV>
+__device__ __noinline__ float4 wide_sums_bf16(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const __nv_bfloat16* x, int64_t ldx, int vec_x, int columns, int per_token, int first, int k) {
     uint32_t fa[2], fb[2], more_a = 0x3F803F80u, more_b = 0x3F803F80u;
     if constexpr (NV) {                                 // 2^118 times the scales: 2^126 times 448 would be too large
 #pragma unroll
@@ -147,11 +184,12 @@ __device__ __noinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32
         if (ca != 255u && ca > 128u) more_a = (ca - 1u) * 0x00800080u;
         if (cb != 255u && cb > 128u) more_b = (cb - 1u) * 0x00800080u;
     }
-    const int c = first + (int(threadIdx.x & 31) >> 2), tok = c / per_token, part = c % per_token;      // (parts of nothing are zeros)
+    const int c = first + (int(threadIdx.x & 31) >> 2), tok = c / per_token;
+    const bool there = k >= 0 && c < columns && c % per_token == 0;     // (a token's other columns: zeros)
     float d[4] = {};
 #pragma unroll 1
     for (int word = 0; word < 4; ++word) {
-        uint32_t ra[4], rb[4], u[8];
+        uint32_t ra[4], rb[4];
         decode_bf16(word_of(va, word), ra);
         decode_bf16(word_of(vb, word), rb);
 #pragma unroll
@@ -159,19 +197,10 @@ __device__ __noinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32
             ra[j] = mul_bf16x2(mul_bf16x2(ra[j], fa[word >> 1]), more_a);
             rb[j] = mul_bf16x2(mul_bf16x2(rb[j], fb[word >> 1]), more_b);
         }
-        Pair v[4];
-        widen<T>(load8<T, false>(x + (k >= 0 && c < columns ? tok * ldx + k + word * 8 : 0), k >= 0 && c < columns ? 8 : 0, vec_x), v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {                   // the column's part: truncations of what is left; an infinity or NaN is the first alone
-            float even, odd;
-            split(v[i / 2], even, odd);
-            u[i] = __float_as_uint(i & 1 ? odd : even);
-            const bool number = (u[i] & INF_BITS) != INF_BITS;
-            for (int p = 0; p < part; ++p) u[i] = number ? __float_as_uint(__fsub_rn(__uint_as_float(u[i]), __uint_as_float(u[i] & 0xFFFF0000u))) : 0u;
-            u[i] = u[i] >> 16 | (!number && part == 0 && (u[i] & 0xFFFFu) ? 0x40u : 0u);
-        }
-        mma<true>(d, ra[0], rb[0], ra[1], rb[1], u[0] | u[4] << 16, u[1] | u[5] << 16);
-        mma<true>(d, ra[2], rb[2], ra[3], rb[3], u[2] | u[6] << 16, u[3] | u[7] << 16);
+        const Raw<EF_BF16> v = load8<EF_BF16, false>(x + (there ? tok * ldx + k + word * 8 : 0), there ? 8 : 0, vec_x);
+        // (the codes' order: elements j and j + 4 side by side)
+        mma<true>(d, ra[0], rb[0], ra[1], rb[1], __byte_perm(v.w[0], v.w[2], 0x5410), __byte_perm(v.w[0], v.w[2], 0x7632));
+        mma<true>(d, ra[2], rb[2], ra[3], rb[3], __byte_perm(v.w[1], v.w[3], 0x5410), __byte_perm(v.w[1], v.w[3], 0x7632));
     }
     constexpr float back = NV ? 256.0f : 1.0f;
     return make_float4(d[0] * back, d[1] * back, d[2] * back, d[3] * back);
@@ -448,19 +477,18 @@ __device__ __forceinline__ bool stage_x(const Raw<T>& raw, unsigned char* at, in
         // the parts behind would show it).
         const int up = min(141 - int(top >> 23), 126 - 12 * (P - 1));
         const Pair f = both(__uint_as_float(uint32_t(max(up, -126) + 127) << 23));
-        uint32_t lost = up >= -16 && top < INF_BITS ? 0u : 1u, half[P][4];
+        uint32_t lost = up >= -16 && top < INF_BITS ? 0u : 1u, half[P][4], least = 0xFFFFFFFFu;           // least: of the magnitudes but zero, as bits, less one
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float even, odd;
+            float even, odd, x0, x1;
+            split(p[j], x0, x1);
             split(mul2(p[j], f), even, odd);
-            if constexpr (T == EF_F32) {                // (a subnormal number times 2^up may lose bits)
-                float x0, x1;
-                split(p[j], x0, x1);
-                lost |= uint32_t(even == 0.0f && x0 != 0.0f) | uint32_t(odd == 0.0f && x1 != 0.0f);
-            }
+            least = __viaddmin_u32(__float_as_uint(x0) & 0x7FFFFFFFu, 0xFFFFFFFFu, least);
+            least = __viaddmin_u32(__float_as_uint(x1) & 0x7FFFFFFFu, 0xFFFFFFFFu, least);
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(half[q][j]) : "f"(odd), "f"(even));
+                if (P == 1) continue;                   // (a normal FP16 number has all bits of a BF16 one)
                 const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&half[q][j]));
                 if (q == P - 1) lost |= (__float_as_uint(even) ^ __float_as_uint(back.x)) | (__float_as_uint(odd) ^ __float_as_uint(back.y));
                 else {
@@ -469,6 +497,7 @@ __device__ __forceinline__ bool stage_x(const Raw<T>& raw, unsigned char* at, in
                 }
             }
         }
+        lost |= uint32_t(least < (P > 1 || up < 113 ? uint32_t(113 - up) << 23 : 1u << (135 - up)) - 1u);          // times 2^up below 2^-14
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             *reinterpret_cast<uint4*>(at + q * pitch) = make_uint4(half[q][0], half[q][1], half[q][2], half[q][3]);
@@ -610,6 +639,13 @@ struct Kernel {
         return lost;
     }
 
+    __device__ __forceinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, int first, int k) const {
+        const E* x = static_cast<const E*>(a.x);
+        if constexpr (T == EF_F32) return wide_sums_f32<NV>(va, vb, ca, cb, x, a.ldx, a.tokens, first, k);
+        else if constexpr (T == EF_BF16) return wide_sums_bf16<NV>(va, vb, ca, cb, x, a.ldx, a.vec_x, a.tokens * PER_TOKEN, PER_TOKEN, first, k);
+        else return make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // (FP16 is always exact)
+    }
+
     // The tile's shares of its warps, put together.
     __device__ __forceinline__ float row_scale(const Walk& now) const {        // of the row that this thread puts together (the same one for every token)
         const int first = threadIdx.x - warp / now.split * now.split * 32;
@@ -703,8 +739,7 @@ struct Kernel {
                         const int k = step * STEP + h * HALF + t * 32;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
-                            product.add(nt, wide_sums<T, NV>(h ? va[1] : va[0], h ? vb[1] : vb[0], h ? codes[1][0] : codes[0][0], h ? codes[1][1] : codes[0][1], static_cast<const E*>(a.x), a.ldx,
-                                                             a.vec_x, a.tokens * PER_TOKEN, PER_TOKEN, nt * 8, k < a.K ? k : -1));
+                            product.add(nt, wide_sums(h ? va[1] : va[0], h ? vb[1] : vb[0], h ? codes[1][0] : codes[0][0], h ? codes[1][1] : codes[0][1], nt * 8, k < a.K ? k : -1));
                     }
                 } else if constexpr (BLOCKS) product.step(va, vb, codes);
                 else {
