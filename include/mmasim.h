@@ -271,10 +271,12 @@ int mmasim_quantize(int in_fmt, int out_fmt, int64_t M, int64_t K, const void* x
 
 /* Root-mean-square norm, with the residual's addition in front and quantisation behind:
  *   h = x + residual, one rounding to the rows' type, stored to residual_out (x itself without a residual; both or neither are given)
- *   y = fl(fl(h / sqrt(mean of h^2 + eps)) * weight), the sum of squares in FP32; rounded once to the rows' type (out_fmt = fmt), or
- *       quantised from FP32 as above (sf and row_scale as the format has them)
- * A row whose sum of squares passes FP32's range (magnitudes of 1.8e19 and more) comes out as zeros.  residual_out may be x or residual (same
- * address and stride), and so may a plain `out` be. */
+ *   y = (h r) * weight, r = 1 / sqrt(mean of h^2 + eps), in FP32: the sum of squares in an order of the kernel's own, r within 2^-23 of the root
+ *       of it, two rounded products; rounded once to the rows' type (out_fmt = fmt), or quantised from FP32 as above (sf and row_scale as the
+ *       format has them)
+ * The squares are FP32 numbers too.  A row whose sum of them passes FP32's range comes out as zeros: K magnitudes of 1.8e19 / sqrt(K), 2.9e17 for
+ * K = 4096.  With eps = 0 a row whose mean square is below 2^-126 (magnitudes below 1e-19) loses bits, and one whose squares are all zero
+ * (magnitudes below 2^-75) comes out as NaN.  residual_out may be x or residual (same address and stride), and so may a plain `out` be. */
 typedef struct {
     const void* x;
     const void* residual;       /* or NULL */
@@ -293,9 +295,11 @@ int mmasim_rms_norm(int fmt, int64_t M, int64_t K, const mmasim_rms_norm_args* a
 /* Its gradients, a quantised output taken as if it were not (straight through).  With r = 1 / sqrt(mean of h^2 + eps) and g = dy * weight:
  *   dx = r (g - (h r) (r / K) sum(g h)) + dresidual     the gradient of x and of residual alike, one rounding to the rows' type
  *   dweight = sum over the rows of dy h r           one rounding to weight_fmt; zeros for M = 0
- * h is what the forward pass stored (residual_out, or x).  dweight is the same from run to run: the rows are added in a fixed order, through
- * `workspace` (device, mmasim_rms_norm_backward_workspace(M, K) bytes, 16-byte aligned; not needed without dweight), whose contents before
- * and after mean nothing; calls that may run at the same time need one each.  dx may be dy, h or dresidual (same address and stride). */
+ * Both sums of a row are FP32 sums, with the limits that the norm has (beyond the upper one dx is dresidual, or zeros, and the row adds nothing
+ * to dweight); products g h below 2^-126 lose bits.  h is what the forward pass stored (residual_out, or x).  dweight is the same from run to
+ * run: the rows are added in a fixed order, through `workspace` (device, mmasim_rms_norm_backward_workspace(M, K) bytes, 16-byte aligned; not
+ * needed without dweight), whose contents before and after mean nothing; calls that may run at the same time need one each.  dx may be dy, h or
+ * dresidual (same address and stride). */
 typedef struct {
     const void* dy;
     const void* h;
@@ -319,8 +323,8 @@ int mmasim_rms_norm_backward(int fmt, int64_t M, int64_t K, const mmasim_rms_nor
  * 0 = K), sf N x K / 32 E8M0 or N x K / 16 UE4M3 bytes; row_scale N floats or NULL.  fmt: x and y, FP32, BF16 or FP16.  K a multiple of 32.
  * Products of x, code and scale are exact, sums FP32 (over 128 elements by the matrix instruction, which truncates below 2^-24 of the largest
  * term, an FP16 x below 2^-14 taken for 2^-14 there, then by rounded additions in a fixed order), one rounding to the type of y.  Weights of
- * 2^128 and more (E8M0 codes 253 and 254) may come out infinite, and then NaN times zeros of x.  T >= 0; up to 16 tokens of 16 bits or five of FP32 (fewer where K is too long for their place in shared memory) read the
- * weights together.  K up to 32768, FP32 20480. */
+ * 2^128 and more before row_scale (E8M0 codes 253 and 254) may come out infinite, and then NaN times zeros of x.  T >= 0; up to 16 tokens of 16
+ * bits or five of FP32 (fewer where K is too long for their place in shared memory) read the weights together.  K up to 32768, FP32 20480. */
 int mmasim_matvec4(int w_fmt, int fmt, int64_t T, int64_t N, int64_t K, const void* W, int64_t ldw, const void* sf, const float* row_scale,
                    const void* x, int64_t ldx, void* y, int64_t ldy, void* stream);
 

@@ -5,7 +5,8 @@
 //   row scales   s = max(max |y| / top, 2^-126), code = nearest(y / s)                                   E4M3, E5M2
 //   blocks of 32 sf = floor(log2 max |y|) - emax (E8M0), code = nearest(y / 2^sf)                          MXE4M3, MXE5M2, MXF4
 //   blocks of 16 s = max(row's max |y| / 2688, 2^-100), g = nearest UE4M3 of max |y| / 6s, code = nearest(y / gs)     NVF4
-// with FP32 roundings in between, as plain FP32 arithmetic has them (the sum of squares is the one value whose order is the kernel's own).
+// with FP32 roundings in between: scales and quotients as plain FP32 arithmetic has them (Divisor), y as (h r) w with the mean from fl(1 / K), the
+// sum of squares in the kernel's own order and r within 2^-23 (inverse_root).
 //
 // What bounds it is memory: 7 bytes an element for BF16 with a residual into FP8.  A row is `threads` threads (8, 16 or
 // 32 of a warp, or a CTA), each with V eights of consecutive elements `threads` eights apart, so that a warp's loads are contiguous and a

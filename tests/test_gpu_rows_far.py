@@ -61,3 +61,30 @@ def test_small_gradients_of_large_rows(K):
     dx, _ = mmasim.rms_norm_backward(dy.cuda(), (h * 8).cuda())
     dx64, _, bound, _ = ref.rms_norm_backward(np64(dy), np64(h * 8), None, None, 1e-6)
     assert (np.abs(np64(dx) - dx64) <= bound + ref.U * (np.abs(dx64) + bound)).all()
+
+
+def test_where_the_squares_leave_fp32():
+    """A row of 4096 elements passes FP32's range of squares at magnitudes of 2.9e17, far below one element's 1.8e19."""
+    K = 4096
+    sign = torch.where(torch.rand((4, K), generator=torch.Generator().manual_seed(1)) < 0.5, -1.0, 1.0)
+    h = (sign * torch.tensor([[1e17], [2.8e17], [3.0e17], [1e19]])).cuda()
+    y, _ = mmasim.rms_norm(h)
+    assert (y[2:] == 0).all() and (y[:2].cpu() - sign[:2]).abs().max() <= 2 * ref.NORM_REL
+    dy, res = torch.randn((4, K), generator=torch.Generator().manual_seed(2)).cuda(), torch.randn((4, K), generator=torch.Generator().manual_seed(3)).cuda()
+    dx, dw = mmasim.rms_norm_backward(dy, h, None, res)
+    assert torch.equal(dx[2:], res[2:])
+    assert torch.equal(dw, mmasim.rms_norm_backward(dy[:2], h[:2])[1])
+    assert (mmasim.rms_norm_backward(dy, h)[0][2:] == 0).all()
+
+
+def test_small_rows_without_eps():
+    """Down to mean squares of 2^-126 a row's norm is as good as any; where the squares vanish there is nothing to divide by."""
+    x = torch.randn((3, 500), generator=torch.Generator().manual_seed(5))
+    for mag in (1e-12, 1e-16, 1e-18):
+        h = x * mag
+        y, _ = mmasim.rms_norm(h.cuda(), eps=0.0)
+        y64, _ = ref.rms_norm(np64(h), None, 0.0)
+        # squares below 2^-126 are off by up to 2^-150 each
+        assert (np.abs(np64(y) - y64) <= np.abs(y64) * (ref.NORM_REL + ref.U + 2.0 ** -150 / (np64(h) ** 2).mean(1, keepdims=True))).all(), mag
+    h = torch.tensor([[1e-24, -1e-25, 0.0, 1e-30]]).cuda()
+    assert torch.isnan(mmasim.rms_norm(h, eps=0.0)[0]).all()
