@@ -23,7 +23,7 @@
 // how many tiles are left, so that the last ones are spread over the whole chip.  Every warp has the loads of its next three steps in flight
 // into its own part of shared memory, over the ends of tiles too (28672 x 8192: 49 us with these asynchronous copies where loads into registers,
 // as far ahead, took 66).
-// Where it ends: 28672 x 8192 NVFP4, one token, 29.4 us, 0.69 of the copy rate (the copies alone 25.7: 2.5 us until x is staged and the first
+// Where it ends: 28672 x 8192 NVFP4, one token, 29.5 us, 0.69 of the copy rate (the copies alone 25.7: 2.5 us until x is staged and the first
 // tile begun, 7 % for tiles that do not fill the last round; then 2.6 instructions per clock and scheduler quarter).
 #include <type_traits>
 #include "mmasim_quant.cuh"
