@@ -141,6 +141,7 @@ __device__ __forceinline__ float code_value(uint32_t c) { return __fmul_rn(__uin
 template <bool NV>
 __device__ __noinline__ float4 wide_sums_f32(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const float* x, int64_t ldx, int tokens, int first, int k) {
     constexpr int P = PARTS<EF_F32>;
+    if (k < 0) va = vb = make_uint4(0u, 0u, 0u, 0u);     // (a block behind the last is the last again: infinite weights times zeros would be NaN)
     float d[4] = {};
 #pragma unroll 1
     for (int tok = (first + P - 1) / P; tok < tokens && tok * P < first + 8; ++tok) {
@@ -169,8 +170,9 @@ __device__ __noinline__ float4 wide_sums_f32(uint4 va, uint4 vb, uint32_t ca, ui
     return make_float4(d[0], d[1], d[2], d[3]);
 }
 // BF16, through the instruction.
-template <bool NV>
-__device__ __noinline__ float4 wide_sums_bf16(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const __nv_bfloat16* x, int64_t ldx, int vec_x, int columns, int per_token, int first, int k) {
+template <bool NV, int PER_TOKEN>
+__device__ __noinline__ float4 wide_sums_bf16(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, const __nv_bfloat16* x, int64_t ldx, int vec_x, int tokens, int first, int k) {
+    if (k < 0) va = vb = make_uint4(0u, 0u, 0u, 0u);
     uint32_t fa[2], fb[2], more_a = 0x3F803F80u, more_b = 0x3F803F80u;
     if constexpr (NV) {                                 // 2^118 times the scales: 2^126 times 448 would be too large
 #pragma unroll
@@ -184,8 +186,8 @@ __device__ __noinline__ float4 wide_sums_bf16(uint4 va, uint4 vb, uint32_t ca, u
         if (ca != 255u && ca > 128u) more_a = (ca - 1u) * 0x00800080u;
         if (cb != 255u && cb > 128u) more_b = (cb - 1u) * 0x00800080u;
     }
-    const int c = first + (int(threadIdx.x & 31) >> 2), tok = c / per_token;
-    const bool there = k >= 0 && c < columns && c % per_token == 0;     // (a token's other columns: zeros)
+    const int c = first + (int(threadIdx.x & 31) >> 2), tok = c / PER_TOKEN;
+    const bool there = k >= 0 && tok < tokens && c % PER_TOKEN == 0;     // (a token's other columns: zeros)
     float d[4] = {};
 #pragma unroll 1
     for (int word = 0; word < 4; ++word) {
@@ -203,7 +205,9 @@ __device__ __noinline__ float4 wide_sums_bf16(uint4 va, uint4 vb, uint32_t ca, u
         mma<true>(d, ra[2], rb[2], ra[3], rb[3], __byte_perm(v.w[1], v.w[3], 0x5410), __byte_perm(v.w[1], v.w[3], 0x7632));
     }
     constexpr float back = NV ? 256.0f : 1.0f;
-    return make_float4(d[0] * back, d[1] * back, d[2] * back, d[3] * back);
+    const int column = 2 * int(threadIdx.x & 3);
+    const bool even = column % PER_TOKEN == 0, odd = (column + 1) % PER_TOKEN == 0;        // (of a column of zeros: NaN, where a weight is infinite)
+    return make_float4(even ? d[0] * back : 0.0f, odd ? d[1] * back : 0.0f, even ? d[2] * back : 0.0f, odd ? d[3] * back : 0.0f);
 }
 // A step whose blocks have scales far apart or far out (or NaN), one block of the four at a time, for eight columns.
 __device__ __noinline__ float4 block_sums(uint4 va, uint4 vb, int ca, int cb, uint32_t x, float2 f) {
@@ -642,7 +646,7 @@ struct Kernel {
     __device__ __forceinline__ float4 wide_sums(uint4 va, uint4 vb, uint32_t ca, uint32_t cb, int first, int k) const {
         const E* x = static_cast<const E*>(a.x);
         if constexpr (T == EF_F32) return wide_sums_f32<NV>(va, vb, ca, cb, x, a.ldx, a.tokens, first, k);
-        else if constexpr (T == EF_BF16) return wide_sums_bf16<NV>(va, vb, ca, cb, x, a.ldx, a.vec_x, a.tokens * PER_TOKEN, PER_TOKEN, first, k);
+        else if constexpr (T == EF_BF16) return wide_sums_bf16<NV, PER_TOKEN>(va, vb, ca, cb, x, a.ldx, a.vec_x, a.tokens, first, k);
         else return make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // (FP16 is always exact)
     }
 

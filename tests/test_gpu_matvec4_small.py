@@ -52,3 +52,17 @@ def test_small_bf16_tokens(fmt, power):
         x[:, 1::3] = 1.0
         codes[:, 1::3] &= 8                 # zeros of both signs
         check(fmt, x, codes, sf, None, ref.HALF_STEP["bf16"], 2.0 ** -134)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_weights_beyond_fp32_in_the_last_block(dtype):
+    """One weight of 6 x 2^127 under an x of 1: infinite, also where lanes behind the last block of a step that FP16 does not hold repeat its weights."""
+    for T in (1, 2, 4, 9):
+        for K in (32, 96, 288, 320):
+            codes = np.zeros((18, K), np.uint8)
+            sf = np.full((18, K // 32), 127, np.uint8)
+            codes[:, K - 5], sf[:, -1] = np.where(np.arange(18) % 2, 7, 15), 254
+            x = torch.ones((T, K))
+            x[:, K - 9], x[:, K - 7] = 1e25, 2.0 ** -45
+            y = mmasim.matvec4("mxf4", torch.from_numpy(ref.pack(codes, "mxf4")).cuda(), torch.from_numpy(sf).cuda(), x.to(ref.DTYPES[dtype]).cuda()).cpu().float()
+            assert torch.equal(y, torch.tensor([-float("inf"), float("inf")]).repeat(T, 9)), (T, K)
